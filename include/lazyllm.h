@@ -522,6 +522,90 @@ int lazyllm_op_gather(const void* h, const int32_t* pos, const int32_t* keep_idx
                       const int32_t* prune_idx, int32_t n_prune, void* h_out, int32_t* pos_out,
                       void* aux_h, int32_t* aux_pos, int32_t d, void* hip_stream);
 
+/* ---- serving a batch from bounded K,V caches ---------------------------------------------------
+ * The steps of a layer that generates for `batch` requests at once after a (pruned) prefill: attention of
+ * the new tokens over per-request caches, optionally behind a prefix that all requests share, and eviction
+ * by Eq. 1's weight accumulated over the steps.  They keep nothing between calls, allocate nothing, do not
+ * synchronise and can be captured into a graph; lengths live on the device, so that a captured step can be
+ * replayed as they grow.  One cache is one layer's; layers can be stacked into the batch for the eviction.
+ *
+ * lazyllm_kv_cache: K and V (device, bf16, 16-byte aligned) of `batch` requests with `capacity` slots each.
+ * Slot s of request b starts batch_stride * b + row_stride * s ELEMENTS behind k (and v) and holds
+ * [n_kv_heads, head_dim].  The order of a request's slots means nothing to the attention.  head_dim 64 or
+ * 128; strides multiples of 8; row_stride from n_kv_heads * head_dim to 2^24; batch_stride at least
+ * row_stride * (capacity - 1) + n_kv_heads * head_dim, so that no two rows overlap (unused with batch 1);
+ * batch * capacity below 2^31.  Rows beyond a request's length are not read. */
+typedef struct lazyllm_kv_cache {
+  void* k;
+  void* v;
+  int64_t batch_stride, row_stride;
+  int32_t batch, capacity, n_kv_heads, head_dim;
+} lazyllm_kv_cache;
+
+/* What a step's attention takes beside the cache.  Pointers are device memory; q, k_new, v_new, o, prefix_k and
+ * prefix_v bf16 and 16-byte aligned.
+ *   lengths   int32 [batch]: tokens in the cache before this step.  Negative: the request takes no part, its
+ *             rows of o are set to zero and its cache and tables are left as they are.
+ *   q_len     new tokens of every request, 1 .. 64.  max_len: the most that a length can be, at least 0, with
+ *             max_len + q_len <= capacity; grids and workspace follow it.  A length beyond it counts as
+ *             max_len and sets LAZYLLM_ST_BAD_CU in *status (int32, may be NULL; bits are only ever added).
+ *   q         [batch, q_len, n_heads, head_dim], rotary applied; n_heads a multiple of n_kv_heads, at most 256.
+ *   k_new,    [batch, q_len, n_kv_heads, head_dim]: K (rotary applied) and V of the new tokens; they are written to
+ *   v_new     the slots from the request's length on.  Neither may lie in the cache.
+ *   o         [batch, q_len, n_heads, head_dim].
+ *   weight,   fp32 [batch, capacity], both or neither: weight_out[b][s] = weight[b][s] + sum over the new tokens of
+ *   weight_out  the mean over all heads of their attention probability at slot s (Eq. 1), for a new token's own
+ *             slot without the first term.  Slots beyond the new length are not written.  May be the same table.
+ *   pos_new,  both or neither: pos_new int32 [batch] is the original position of a request's first new token; the
+ *   pos       new tokens' positions are written into pos int32 [batch, capacity].
+ *   prefix_*  lazyllm_op_prefix_attention only: K and V rows of prefix_len tokens that every request has in front of
+ *             its cache, prefix_stride elements from row to row (as row_stride), e.g. result.k[l], result.v[l] of a
+ *             prefill of the common prompt.
+ * New token t of a request sees the prefix, the request's cached tokens and its new tokens up to t.  Keys and
+ * values that some new token of a request sees must be finite; what lies elsewhere is of no account.
+ * Sums and softmax statistics are fp32; o is rounded once.  The same call gives the same bits every time. */
+typedef struct lazyllm_step_attention {
+  const void *q, *k_new, *v_new;
+  void* o;
+  const int32_t* lengths;
+  int32_t n_heads, q_len, max_len;
+  int32_t prefix_len;
+  const void *prefix_k, *prefix_v;
+  int64_t prefix_stride;
+  const float* weight;
+  float* weight_out;
+  const int32_t* pos_new;
+  int32_t* pos;
+  int32_t* status;
+} lazyllm_step_attention;
+
+/* Bytes of workspace (device, 256-byte aligned) of a step: prefix_len 0 for lazyllm_op_cache_attention; weights:
+ * whether weight_out is given.  Host only.  0 on a bad argument.  Nothing in it needs to be cleared. */
+size_t lazyllm_op_cache_attention_workspace_bytes(const lazyllm_kv_cache* cache, int32_t n_heads, int32_t q_len,
+                                                  int32_t max_len, int32_t prefix_len, int32_t weights);
+
+/* Attention of the new tokens over the requests' own caches; the prefix members of *step are ignored. */
+int lazyllm_op_cache_attention(const lazyllm_kv_cache* cache, const lazyllm_step_attention* step, void* workspace,
+                               size_t ws_bytes, void* hip_stream);
+/* The same behind a common prefix of prefix_len >= 1 tokens, which is read once for all requests. */
+int lazyllm_op_prefix_attention(const lazyllm_kv_cache* cache, const lazyllm_step_attention* step, void* workspace,
+                                size_t ws_bytes, void* hip_stream);
+
+/* Eviction: a request with more than `budget` tokens keeps `budget` of them (the rule of Sec. 3.2 on accumulated
+ * weights): first those whose position is below `sinks` or among the last `recent` positions (above the request's
+ * highest position - recent), then higher weight, then lower slot; a NaN weight is the lowest, -0 is 0.  sinks +
+ * recent <= budget.  Kept tokens in slots below the budget stay there; the others move, in slot order, to the
+ * slots below the budget that became free.  Of K and V only those rows are written; weight_out fp32, pos_out
+ * int32 [batch, capacity] get the tables of the kept tokens (slots 0 .. new length - 1; may be weight and pos
+ * themselves), lengths_out int32 [batch] min(length, budget) (may be lengths), and kept, unless NULL, int32
+ * [batch, budget], the slot that each slot's token was in.  A negative length stays as it is.  A length above
+ * capacity counts as capacity and sets LAZYLLM_ST_BAD_CU in *status (may be NULL).  capacity <= 524288. */
+size_t lazyllm_op_cache_evict_workspace_bytes(const lazyllm_kv_cache* cache, int32_t budget);
+int lazyllm_op_cache_evict(const lazyllm_kv_cache* cache, const float* weight, const int32_t* pos,
+                           const int32_t* lengths, int32_t budget, int32_t sinks, int32_t recent, float* weight_out,
+                           int32_t* pos_out, int32_t* lengths_out, int32_t* kept, int32_t* status, void* workspace,
+                           size_t ws_bytes, void* hip_stream);
+
 /* logits[V] = rmsnorm(h_last, gain) . W_lm^T, fp32 out; xf: device fp32[d] scratch (written only
  * by the two-launch form that rows wider than 32768 elements take). */
 int lazyllm_op_lm_head(const void* h_last, const void* gain, const void* w_lm, float* xf,

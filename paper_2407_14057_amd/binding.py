@@ -79,6 +79,19 @@ class lazyllm_profile_record(C.Structure):
                 ("work", C.c_double)]
 
 
+class lazyllm_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("batch_stride", C.c_int64), ("row_stride", C.c_int64),
+                ("batch", C.c_int32), ("capacity", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class lazyllm_step_attention(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k_new", C.c_void_p), ("v_new", C.c_void_p), ("o", C.c_void_p),
+                ("lengths", C.c_void_p), ("n_heads", C.c_int32), ("q_len", C.c_int32), ("max_len", C.c_int32),
+                ("prefix_len", C.c_int32), ("prefix_k", C.c_void_p), ("prefix_v", C.c_void_p),
+                ("prefix_stride", C.c_int64), ("weight", C.c_void_p), ("weight_out", C.c_void_p),
+                ("pos_new", C.c_void_p), ("pos", C.c_void_p), ("status", C.c_void_p)]
+
+
 STEP_NAMES = ("plan", "rope_table", "embed", "select", "gather", "rmsnorm", "gemm_qkv", "v_transpose",
               "score", "attention", "gemm_o", "gemm_gate_up", "gemm_down", "lm_head")
 
@@ -166,6 +179,16 @@ _SIGNATURES = {
     "lazyllm_op_gather": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
                                     C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                     C.c_int32, C.c_void_p]),
+    "lazyllm_op_cache_attention_workspace_bytes": (C.c_size_t, [C.POINTER(lazyllm_kv_cache), C.c_int32, C.c_int32,
+                                                                C.c_int32, C.c_int32, C.c_int32]),
+    "lazyllm_op_cache_attention": (C.c_int, [C.POINTER(lazyllm_kv_cache), C.POINTER(lazyllm_step_attention),
+                                             C.c_void_p, C.c_size_t, C.c_void_p]),
+    "lazyllm_op_prefix_attention": (C.c_int, [C.POINTER(lazyllm_kv_cache), C.POINTER(lazyllm_step_attention),
+                                              C.c_void_p, C.c_size_t, C.c_void_p]),
+    "lazyllm_op_cache_evict_workspace_bytes": (C.c_size_t, [C.POINTER(lazyllm_kv_cache), C.c_int32]),
+    "lazyllm_op_cache_evict": (C.c_int, [C.POINTER(lazyllm_kv_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                         C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                         C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "lazyllm_op_lm_head": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                      C.c_int32, C.c_int32, C.c_float, C.c_void_p]),
 }
@@ -427,6 +450,58 @@ def lazyllm_op_gather(h, pos, keep_idx, n_keep, prune_idx, n_prune, h_out, pos_o
 def lazyllm_op_lm_head(h_last, gain, w_lm, xf, logits, d, vocab, eps, stream=None) -> None:
     _check(lib().lazyllm_op_lm_head(_ptr(h_last), _ptr(gain), _ptr(w_lm), _ptr(xf), _ptr(logits), d,
                                     vocab, eps, _stream_ptr(stream)))
+
+
+# ---------------------------------------------------------------------------- a batch's K,V caches
+
+def make_kv_cache(k: torch.Tensor, v: torch.Tensor) -> lazyllm_kv_cache:
+    """Descriptor of caches k, v [batch, capacity, n_kv_heads, head_dim] (bf16; strided views of one layout are
+    fine as long as a row's [n_kv_heads, head_dim] is contiguous).  The tensors must outlive it."""
+    if k.shape != v.shape or k.stride() != v.stride() or k.dim() != 4 or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
+        raise LazyLLMError(LAZYLLM_EINVAL)
+    batch, capacity, heads, hd = k.shape
+    if (hd > 1 and k.stride(3) != 1) or (heads > 1 and k.stride(2) != hd):
+        raise LazyLLMError(LAZYLLM_EINVAL)
+    row = k.stride(1) if capacity > 1 else heads * hd          # (the stride of a dimension of one means nothing)
+    return lazyllm_kv_cache(k.data_ptr(), v.data_ptr(), k.stride(0), row, batch, capacity, heads, hd)
+
+
+def lazyllm_op_cache_attention_workspace_bytes(cache: lazyllm_kv_cache, n_heads: int, q_len: int, max_len: int,
+                                               prefix_len: int = 0, weights: bool = False) -> int:
+    return int(lib().lazyllm_op_cache_attention_workspace_bytes(C.byref(cache), n_heads, q_len, max_len, prefix_len,
+                                                                int(weights)))
+
+
+def lazyllm_op_cache_attention(cache, q, k_new, v_new, lengths, n_heads, q_len, max_len, o, workspace, weight=None,
+                               weight_out=None, pos_new=None, pos=None, status=None, stream=None) -> None:
+    s = lazyllm_step_attention(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(o), _ptr(lengths), n_heads, q_len, max_len, 0, None,
+                               None, 0, _ptr(weight), _ptr(weight_out), _ptr(pos_new), _ptr(pos), _ptr(status))
+    _check(lib().lazyllm_op_cache_attention(C.byref(cache), C.byref(s), _ptr(workspace),
+                                            workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+
+
+def lazyllm_op_prefix_attention(cache, prefix_k, prefix_v, q, k_new, v_new, lengths, n_heads, q_len, max_len, o, workspace,
+                                weight=None, weight_out=None, pos_new=None, pos=None, status=None, stream=None) -> None:
+    """prefix_k, prefix_v: [prefix_len, n_kv_heads, head_dim], possibly strided from row to row."""
+    if prefix_k.shape != prefix_v.shape or prefix_k.stride() != prefix_v.stride() or not prefix_k[0].is_contiguous():
+        raise LazyLLMError(LAZYLLM_EINVAL)
+    row = prefix_k.stride(0) if prefix_k.shape[0] > 1 else prefix_k[0].numel()
+    s = lazyllm_step_attention(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(o), _ptr(lengths), n_heads, q_len, max_len,
+                               prefix_k.shape[0], prefix_k.data_ptr(), prefix_v.data_ptr(), row, _ptr(weight),
+                               _ptr(weight_out), _ptr(pos_new), _ptr(pos), _ptr(status))
+    _check(lib().lazyllm_op_prefix_attention(C.byref(cache), C.byref(s), _ptr(workspace),
+                                             workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+
+
+def lazyllm_op_cache_evict_workspace_bytes(cache: lazyllm_kv_cache, budget: int) -> int:
+    return int(lib().lazyllm_op_cache_evict_workspace_bytes(C.byref(cache), budget))
+
+
+def lazyllm_op_cache_evict(cache, weight, pos, lengths, budget, sinks, recent, weight_out, pos_out, lengths_out, workspace,
+                           kept=None, status=None, stream=None) -> None:
+    _check(lib().lazyllm_op_cache_evict(C.byref(cache), _ptr(weight), _ptr(pos), _ptr(lengths), budget, sinks, recent,
+                                        _ptr(weight_out), _ptr(pos_out), _ptr(lengths_out), _ptr(kept), _ptr(status),
+                                        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
 
 
 # ---------------------------------------------------------------------------- decoding steps

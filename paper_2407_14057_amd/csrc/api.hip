@@ -97,6 +97,50 @@ inline int ffn_padded(int f) { return (f + 127) / 128 * 128; }
 inline int kv_heads(const lazyllm_config* c) { return c->n_kv_heads > 0 ? c->n_kv_heads : c->n_heads; }
 inline int kv_dim(const lazyllm_config* c) { return kv_heads(c) * c->head_dim; }
 
+// ---- K,V caches of a batch ------------------------------------------------------------------
+inline bool rows_ok(const void* p) { return p != nullptr && ((uintptr_t)p & 15) == 0; }
+bool row_stride_ok(int64_t stride, int n_kv_heads, int head_dim) {
+  return stride >= (int64_t)n_kv_heads * head_dim && stride <= (1 << 24) && stride % 8 == 0;
+}
+bool kv_cache_shape_ok(const lazyllm_kv_cache* c) {
+  return c != nullptr && (c->head_dim == 64 || c->head_dim == 128) && c->n_kv_heads >= 1 && c->n_kv_heads <= 256 &&
+         c->batch >= 1 && c->batch <= 65535 && c->capacity >= 1 && (int64_t)c->batch * c->capacity <= 0x7fffffff;
+}
+bool kv_cache_ok(const lazyllm_kv_cache* c) {
+  if (!kv_cache_shape_ok(c) || !rows_ok(c->k) || !rows_ok(c->v)) return false;
+  if (!row_stride_ok(c->row_stride, c->n_kv_heads, c->head_dim)) return false;
+  return c->batch == 1 || (c->batch_stride % 8 == 0 && c->batch_stride <= ((int64_t)1 << 45) &&
+                           c->batch_stride >= c->row_stride * (c->capacity - 1) + (int64_t)c->n_kv_heads * c->head_dim);
+}
+bool step_shape_ok(const lazyllm_kv_cache* c, int n_heads, int q_len, int max_len) {
+  return n_heads >= 1 && n_heads <= 256 && n_heads % c->n_kv_heads == 0 && q_len >= 1 && q_len <= 64 && max_len >= 0 &&
+         (int64_t)max_len + q_len <= c->capacity;
+}
+
+int step_attention(const lazyllm_kv_cache* c, const lazyllm_step_attention& s, void* workspace, size_t ws_bytes, hipStream_t st) {
+  if (!kv_cache_ok(c) || !step_shape_ok(c, s.n_heads, s.q_len, s.max_len)) return LAZYLLM_EINVAL;
+  if (!rows_ok(s.q) || !rows_ok(s.k_new) || !rows_ok(s.v_new) || !rows_ok(s.o) || !s.lengths) return LAZYLLM_EINVAL;
+  if ((s.weight == nullptr) != (s.weight_out == nullptr) || (s.pos == nullptr) != (s.pos_new == nullptr)) return LAZYLLM_EINVAL;
+  const CacheAttentionPlan plan = cache_attention_plan(c->batch, s.n_heads, c->n_kv_heads, c->head_dim, s.q_len, s.max_len,
+                                                       s.prefix_len, s.weight != nullptr);
+  if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0) return LAZYLLM_EINVAL;
+  if (ws_bytes < plan.bytes()) return LAZYLLM_ENOSPC;
+  CacheAttentionArgs a{};
+  a.k = (uint16_t*)c->k; a.v = (uint16_t*)c->v;
+  a.batch_stride = c->batch > 1 ? c->batch_stride : 0; a.row_stride = c->row_stride;
+  a.batch = c->batch; a.capacity = c->capacity; a.n_heads = s.n_heads; a.n_kv = c->n_kv_heads;
+  a.q_len = s.q_len; a.max_len = s.max_len;
+  a.q = (const uint16_t*)s.q; a.k_new = (const uint16_t*)s.k_new; a.v_new = (const uint16_t*)s.v_new;
+  a.lengths = s.lengths;
+  a.prefix_k = (const uint16_t*)s.prefix_k; a.prefix_v = (const uint16_t*)s.prefix_v;
+  a.prefix_stride = s.prefix_stride; a.prefix_len = s.prefix_len;
+  a.o = (uint16_t*)s.o;
+  a.weight = s.weight; a.weight_out = s.weight_out;
+  a.pos_new = s.pos_new; a.pos = s.pos; a.status = s.status;
+  LZ_HIP(launch_cache_attention(a, plan, c->head_dim, workspace, st));
+  return LAZYLLM_OK;
+}
+
 bool schedule_ok(int n_layers, const lazyllm_keep* sched, int n_sched) {
   if (n_sched < 0 || n_sched > LAZYLLM_MAX_LAYERS) return false;
   if (n_sched > 0 && sched == nullptr) return false;
@@ -1342,6 +1386,55 @@ int lazyllm_op_gather(const void* h, const int32_t* pos, const int32_t* keep_idx
   if (n_prune > 0 && (!prune_idx || !aux_h || !aux_pos)) return LAZYLLM_EINVAL;
   LZ_HIP(launch_gather(h, pos, keep_idx, n_keep, prune_idx, n_prune, h_out, pos_out, aux_h, aux_pos,
                        d, (hipStream_t)hip_stream));
+  return LAZYLLM_OK;
+}
+
+size_t lazyllm_op_cache_attention_workspace_bytes(const lazyllm_kv_cache* c, int32_t n_heads, int32_t q_len,
+                                                  int32_t max_len, int32_t prefix_len, int32_t weights) {
+  if (!kv_cache_shape_ok(c) || !step_shape_ok(c, n_heads, q_len, max_len) || prefix_len < 0) return 0;
+  return align_up(cache_attention_plan(c->batch, n_heads, c->n_kv_heads, c->head_dim, q_len, max_len, prefix_len,
+                                       weights != 0).bytes() + 1);
+}
+
+int lazyllm_op_cache_attention(const lazyllm_kv_cache* cache, const lazyllm_step_attention* step, void* workspace,
+                               size_t ws_bytes, void* hip_stream) {
+  if (step == nullptr) return LAZYLLM_EINVAL;
+  lazyllm_step_attention s = *step;
+  s.prefix_len = 0;
+  s.prefix_k = s.prefix_v = nullptr;
+  return step_attention(cache, s, workspace, ws_bytes, (hipStream_t)hip_stream);
+}
+
+int lazyllm_op_prefix_attention(const lazyllm_kv_cache* cache, const lazyllm_step_attention* step, void* workspace,
+                                size_t ws_bytes, void* hip_stream) {
+  if (step == nullptr || step->prefix_len < 1 || !rows_ok(step->prefix_k) || !rows_ok(step->prefix_v) || cache == nullptr ||
+      !row_stride_ok(step->prefix_stride, cache->n_kv_heads, cache->head_dim))
+    return LAZYLLM_EINVAL;
+  return step_attention(cache, *step, workspace, ws_bytes, (hipStream_t)hip_stream);
+}
+
+size_t lazyllm_op_cache_evict_workspace_bytes(const lazyllm_kv_cache* c, int32_t budget) {
+  if (!kv_cache_shape_ok(c) || budget < 1 || c->capacity > EVICT_MAX_CAPACITY) return 0;
+  return evict_workspace_bytes(c->batch, c->capacity, budget);
+}
+
+int lazyllm_op_cache_evict(const lazyllm_kv_cache* c, const float* weight, const int32_t* pos,
+                           const int32_t* lengths, int32_t budget, int32_t sinks, int32_t recent, float* weight_out,
+                           int32_t* pos_out, int32_t* lengths_out, int32_t* kept, int32_t* status, void* workspace,
+                           size_t ws_bytes, void* hip_stream) {
+  if (!kv_cache_ok(c) || c->capacity > EVICT_MAX_CAPACITY || !weight || !pos || !lengths || !weight_out || !pos_out ||
+      !lengths_out || budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget)
+    return LAZYLLM_EINVAL;
+  if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0) return LAZYLLM_EINVAL;
+  if (ws_bytes < evict_workspace_bytes(c->batch, c->capacity, budget)) return LAZYLLM_ENOSPC;
+  EvictArgs a{};
+  a.k = (uint16_t*)c->k; a.v = (uint16_t*)c->v;
+  a.batch_stride = c->batch_stride; a.row_stride = c->row_stride;
+  a.batch = c->batch; a.capacity = c->capacity; a.row_chunks = c->n_kv_heads * c->head_dim / 8;
+  a.weight = weight; a.pos = pos; a.lengths = lengths;
+  a.budget = budget; a.sinks = sinks; a.recent = recent;
+  a.weight_out = weight_out; a.pos_out = pos_out; a.lengths_out = lengths_out; a.kept = kept; a.status = status;
+  LZ_HIP(launch_cache_evict(a, workspace, (hipStream_t)hip_stream));
   return LAZYLLM_OK;
 }
 

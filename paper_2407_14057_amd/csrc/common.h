@@ -336,6 +336,56 @@ size_t decode_attention_workspace_bytes(int d_model, int n_heads);
 int decode_key_splits(int M, int n_keys, int n_heads, int head_dim, size_t split_ws_bytes);
 // (the ticket counters at its end must be zero before the first attention launch: launch_gen_embed)
 
+// ---- a batch's K,V caches (cache_attention.hip, cache_evict.hip) --------------------------
+// Strides in elements; slot s of request b starts at b * batch_stride + s * row_stride.
+struct CacheAttentionArgs {
+  uint16_t *k, *v;
+  long long batch_stride, row_stride;
+  int batch, capacity, n_heads, n_kv, q_len, max_len;
+  const uint16_t *q, *k_new, *v_new;
+  const int32_t* lengths;
+  const uint16_t *prefix_k, *prefix_v;
+  long long prefix_stride;
+  int prefix_len;
+  uint16_t* o;
+  const float* weight;
+  float* weight_out;
+  const int32_t* pos_new;
+  int32_t* pos;
+  int32_t* status;
+  // filled in by the launcher
+  int group, own_blocks, own_range, own_parts, prefix_blocks, prefix_range, prefix_parts, merge, z_ld;
+  float scale_log2e;
+  float* part;                         // [parts][rows][head_dim], rows = batch * q_len * n_heads
+  float2* stat;                        // [parts][rows] (maximum, sum), base 2
+  float* z;                            // [rows][z_ld] base-2 logits against the own cache
+};
+struct CacheAttentionPlan {
+  int tiles;                           // 16-row tiles of query rows per work item
+  int own_blocks, own_range, own_parts, prefix_blocks, prefix_range, prefix_parts, merge, z_ld;
+  size_t part_bytes, stat_bytes, z_bytes;
+  size_t bytes() const { return part_bytes + stat_bytes + z_bytes; }
+};
+CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int head_dim, int q_len, int max_len,
+                                        int prefix_len, bool weights);
+hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan& plan, int head_dim, void* workspace, hipStream_t st);
+
+constexpr int EVICT_MAX_CAPACITY = 1 << 19;          // two bits a slot in the 160 KB of LDS
+struct EvictArgs {
+  uint16_t *k, *v;
+  long long batch_stride, row_stride;
+  int batch, capacity, row_chunks;     // row_chunks: 16-byte pieces of a row
+  const float* weight;
+  const int32_t *pos, *lengths;
+  int budget, sinks, recent;
+  float* weight_out;
+  int32_t *pos_out, *lengths_out, *kept, *status;
+  int32_t* moves;                      // workspace: [batch] counts, then per request holes[max_moves], movers[max_moves]
+  int max_moves;
+};
+size_t evict_workspace_bytes(int batch, int capacity, int budget);
+hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st);
+
 struct PlanArgs {
   int32_t n_stages;                     // pruning stages after stage 0
   int32_t permille[128];                // keep ratio entering stage s+1

@@ -1,0 +1,503 @@
+"""A batch's K,V caches on the GPU: attention of the new tokens (with and without a shared prefix), Eq. 1's weights kept up to
+date, eviction.  Against plain implementations in 64 bits; everything that must not be read holds NaN."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2407_14057_amd import binding as B
+from paper_2407_14057_amd import synth
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+NAN = float("nan")
+
+
+def _bf16(gen, *shape, scale=1.0):
+    return (torch.randn(shape, generator=gen, dtype=torch.float32) * scale).to(torch.bfloat16).to(DEV)
+
+
+class Step:
+    """One step's inputs.  Cached rows beyond a request's length, the whole cache of an idle request and the workspace are NaN."""
+
+    def __init__(self, heads, lengths, q_len, prefix=0, slack=3, seed=0, spread=1.5, interleaved=False, max_len=None, weights=True):
+        self.H, self.kvh, self.hd = heads
+        self.lengths, self.q_len, self.prefix, self.weights = list(lengths), q_len, prefix, weights
+        self.batch = len(self.lengths)
+        self.max_len = max(0, max(self.lengths)) if max_len is None else max_len
+        self.capacity = self.max_len + q_len + slack
+        g = torch.Generator().manual_seed(seed)
+        kv = torch.full((self.batch, self.capacity, 2, self.kvh, self.hd), NAN, dtype=torch.bfloat16, device=DEV)
+        self.k, self.v = (kv[:, :, 0], kv[:, :, 1]) if interleaved else (kv[:, :, 0].contiguous(), kv[:, :, 1].contiguous())
+        self.weight = torch.full((self.batch, self.capacity), NAN, device=DEV)
+        for b, n in enumerate(self.lengths):
+            n = max(n, 0)
+            self.k[b, :n], self.v[b, :n] = _bf16(g, n, self.kvh, self.hd), _bf16(g, n, self.kvh, self.hd)
+            self.weight[b, :n] = torch.rand(n, generator=g).to(DEV) / max(n, 1)
+        self.q = _bf16(g, self.batch, q_len, self.H, self.hd, scale=spread)
+        self.k_new, self.v_new = _bf16(g, self.batch, q_len, self.kvh, self.hd), _bf16(g, self.batch, q_len, self.kvh, self.hd)
+        self.pk, self.pv = _bf16(g, prefix, self.kvh, self.hd), _bf16(g, prefix, self.kvh, self.hd)
+        self.len_dev = torch.tensor(self.lengths, dtype=torch.int32, device=DEV)
+        self.pos = torch.full((self.batch, self.capacity), -7, dtype=torch.int32, device=DEV)
+        self.pos_new = torch.tensor([10 * b + max(n, 0) for b, n in enumerate(self.lengths)], dtype=torch.int32, device=DEV)
+        self.o = torch.full_like(self.q, NAN)
+        self.weight_out = torch.full_like(self.weight, -5.0)
+        self.status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        self.cache = B.make_kv_cache(self.k, self.v)
+        size = B.lazyllm_op_cache_attention_workspace_bytes(self.cache, self.H, q_len, self.max_len, prefix, weights)
+        assert size > 0
+        self.ws = torch.full((size,), 255, dtype=torch.uint8, device=DEV)
+
+    def run(self, stream=None, in_place=False):
+        more = dict(pos_new=self.pos_new, pos=self.pos, status=self.status, stream=stream)
+        if self.weights:
+            more.update(weight=self.weight, weight_out=self.weight if in_place else self.weight_out)
+        args = (self.q, self.k_new, self.v_new, self.len_dev, self.H, self.q_len, self.max_len, self.o, self.ws)
+        if self.prefix:
+            B.lazyllm_op_prefix_attention(self.cache, self.pk, self.pv, *args, **more)
+        else:
+            B.lazyllm_op_cache_attention(self.cache, *args, **more)
+
+    def expected(self):
+        """(o, sum of p |v|, added weights per slot [batch, capacity], largest sum of |q_i k_i| / sqrt(hd)) in 64 bits."""
+        group = self.H // self.kvh
+        o = torch.zeros(self.q.shape, dtype=torch.float64, device=DEV)
+        size = torch.zeros_like(o)
+        add = torch.zeros(self.batch, self.capacity, dtype=torch.float64, device=DEV)
+        reach = 0.0
+        for b, n in enumerate(self.lengths):
+            if n < 0:
+                continue
+            n = min(n, self.max_len)
+            k = torch.cat([self.pk, self.k[b, :n], self.k_new[b]]).double().repeat_interleave(group, dim=1).transpose(0, 1).contiguous()
+            v = torch.cat([self.pv, self.v[b, :n], self.v_new[b]]).double().repeat_interleave(group, dim=1).transpose(0, 1).contiguous()
+            q = self.q[b].double().transpose(0, 1).contiguous()                                    # [H, Q, hd]
+            kt = k.transpose(1, 2).contiguous()
+            z = torch.matmul(q, kt) / math.sqrt(self.hd)
+            reach = max(reach, float((torch.matmul(q.abs(), kt.abs()) / math.sqrt(self.hd)).max()))
+            key = torch.arange(k.shape[1], device=DEV)
+            seen = key[None, :] <= self.prefix + n + torch.arange(self.q_len, device=DEV)[:, None]
+            p = torch.softmax(z.masked_fill(~seen, -math.inf), dim=-1)
+            o[b] = torch.matmul(p, v).transpose(0, 1)
+            size[b] = torch.matmul(p, v.abs()).transpose(0, 1)
+            add[b, :n + self.q_len] = p[:, :, self.prefix:].sum((0, 1)) / self.H
+        return o, size, add, reach
+
+    def check(self, k_before, v_before, weight_before, weight_got):
+        o, size, add, reach = self.expected()
+        # a probability: hd fp32 roundings of a logit's products and sums, twice (its own and the sum's below), the
+        # exponential, and the two bf16 terms that it goes into the second product as; sums of up to n terms
+        keys = self.prefix + self.max_len + self.q_len
+        rel = 2 * (self.hd + 4) * 2.0 ** -24 * max(reach, 1.0) + 2.0 ** -16 + keys * 2.0 ** -24
+        err = (self.o.double() - o).abs()
+        bound = o.abs() * 2.0 ** -8 + size * rel + 1e-30
+        assert bool((err <= bound).all()), (float((err / bound).max()), rel)
+        for b, n in enumerate(self.lengths):
+            if n < 0:
+                assert not self.o[b].any()
+                end = 0
+            else:
+                n = min(n, self.max_len)
+                end = n + self.q_len
+                for got, before, new in ((self.k, k_before, self.k_new), (self.v, v_before, self.v_new)):
+                    assert torch.equal(got[b, :n], before[b, :n]) and torch.equal(got[b, n:end], new[b])
+                assert self.pos[b, n:end].tolist() == list(range(int(self.pos_new[b]), int(self.pos_new[b]) + self.q_len))
+                assert bool((self.pos[b, :n] == -7).all())
+                if self.weights:
+                    before = torch.cat([weight_before[b, :n], torch.zeros(self.q_len, device=DEV)]).double()
+                    want = before + add[b, :end]
+                    tol = add[b, :end] * rel + want * 2.0 ** -23 + 1e-30
+                    err = (weight_got[b, :end].double() - want).abs()
+                    assert bool((err <= tol).all()), (b, float((err / tol).max()))
+            assert bool(self.k[b, end:].isnan().all()) and bool(self.v[b, end:].isnan().all())
+            assert bool((self.pos[b, end:] == -7).all())
+
+    def run_and_check(self, in_place=False, stream=None):
+        k, v, w = self.k.clone(), self.v.clone(), self.weight.clone()
+        torch.cuda.synchronize()
+        self.run(in_place=in_place, stream=stream)
+        torch.cuda.synchronize()
+        self.check(k, v, w, self.weight if in_place else self.weight_out)
+        if self.weights and not in_place:
+            for b, n in enumerate(self.lengths):
+                end = 0 if n < 0 else min(n, self.max_len) + self.q_len
+                assert bool((self.weight_out[b, end:] == -5.0).all())
+
+
+HEADS = {"4x64": (4, 4, 64), "4/2x64": (4, 2, 64), "32/8x128": (32, 8, 128), "8/1x128": (8, 1, 128), "9/3x64": (9, 3, 64), "2x128": (2, 2, 128)}
+EDGES = [0, 1, 15, 16, 17, 31, 32, 33, -1, 63, 95, 127, 128, 129, 255, 256, 257, 300]
+
+
+@pytest.mark.parametrize("heads", list(HEADS))
+@pytest.mark.parametrize("q_len", [1, 2, 5, 17, 64])
+def test_attention_over_caches_of_every_length(heads, q_len):
+    Step(HEADS[heads], EDGES, q_len, seed=q_len).run_and_check(in_place=q_len == 2)
+
+
+@pytest.mark.parametrize("heads,lengths,q_len", [("4x64", [1], 1), ("4x64", [0], 3), ("32/8x128", [5000, 1, 4097, 777], 1),
+                                                 ("2x128", [20000], 1), ("4/2x64", [20011, 3], 4), ("8/1x128", [9001], 7)])
+def test_attention_over_few_and_long_caches(heads, lengths, q_len):
+    Step(HEADS[heads], lengths, q_len, seed=3).run_and_check()
+
+
+def test_attention_of_a_hundred_requests():
+    rng = np.random.default_rng(5)
+    Step((4, 2, 64), [int(x) for x in rng.integers(-1, 700, 130)], 2, seed=4).run_and_check()
+
+
+def test_without_weights_and_alone():
+    """One request that one workgroup per head serves, and the same as part of a batch, without the weights."""
+    for lengths in ([90], [90, 400, -1]):
+        s = Step((4, 4, 64), lengths, 1, seed=8, weights=False)
+        s.run_and_check()
+
+
+def test_all_requests_idle():
+    for weights in (True, False):
+        for max_len in (0, 600):
+            s = Step((4, 2, 64), [-1, -5], 2, seed=8, weights=weights, max_len=max_len)
+            s.run_and_check()
+
+
+@pytest.mark.parametrize("heads", list(HEADS))
+@pytest.mark.parametrize("prefix", [1, 31, 32, 33, 129, 700])
+def test_shared_prefix(heads, prefix):
+    Step(HEADS[heads], [0, 5, -1, 33, 1, 300, 129], 1 + prefix % 3, prefix=prefix, seed=prefix).run_and_check()
+
+
+@pytest.mark.parametrize("heads,batch,q_len", [("4x64", 1, 1), ("4x64", 16, 1), ("4x64", 17, 1), ("2x128", 33, 1), ("32/8x128", 9, 2),
+                                               ("8/1x128", 16, 1), ("8/1x128", 40, 3), ("4/2x64", 130, 1)])
+def test_shared_prefix_by_number_of_query_rows(heads, batch, q_len):
+    rng = np.random.default_rng(batch)
+    lengths = [int(x) for x in rng.integers(0, 60, batch)]
+    Step(HEADS[heads], lengths, q_len, prefix=1111, seed=9, weights=batch % 2 == 0).run_and_check()
+
+
+def test_long_shared_prefix():
+    Step((32, 8, 128), [3, 0, 700], 1, prefix=20003, seed=10).run_and_check()
+
+
+@pytest.mark.parametrize("prefix", [0, 200])
+def test_strided_caches(prefix):
+    """K and V rows interleaved in one buffer, as [slot][2][heads][dim]."""
+    Step((4, 2, 64), [0, 100, 257, -1, 33], 3, prefix=prefix, seed=11, interleaved=True).run_and_check()
+
+
+def test_strided_prefix():
+    s = Step((4, 2, 64), [10, 100], 1, prefix=333, seed=12)
+    both = torch.full((333, 3, 2, 64), NAN, dtype=torch.bfloat16, device=DEV)
+    both[:, 0], both[:, 2] = s.pk, s.pv
+    s.pk, s.pv = both[:, 0], both[:, 2]
+    s.run_and_check()
+
+
+def test_steep_logits():
+    """One key takes nearly everything, and the maximum moves late: the running maximum has to follow."""
+    s = Step((4, 4, 64), [1000, 700], 2, seed=13)
+    s.k[0, 990] = s.q[0, 0] * 4
+    s.k[0, 3] = s.q[0, 1] * 2
+    s.run_and_check()
+    s = Step((4, 4, 64), [1000, 700], 2, seed=14, spread=20.0)
+    s.run_and_check()
+    s = Step((32, 8, 128), [300, 40], 2, prefix=500, seed=15, spread=20.0)
+    s.run_and_check()
+
+
+def test_lengths_above_the_bound_count_as_the_bound():
+    s = Step((4, 2, 64), [50, 400, 20], 2, seed=16, max_len=100, slack=400)
+    s.k[1, :400], s.v[1, :400], s.weight[1, :400] = 0.5, 0.25, 0.125
+    k, v, w = s.k.clone(), s.v.clone(), s.weight.clone()
+    s.run()
+    torch.cuda.synchronize()
+    assert int(s.status) == B.LAZYLLM_ST_BAD_CU
+    s.k[1, 102:], s.v[1, 102:] = NAN, NAN                      # (what lay there was not touched and not read: check() wants NaN)
+    s.check(k, v, w, s.weight_out)
+    t = Step((4, 2, 64), [50, 100, 20], 2, seed=16, max_len=100, slack=400)
+    t.run()
+    torch.cuda.synchronize()
+    assert int(t.status) == 0
+
+
+def test_offsets_beyond_32_bits():
+    """Slots 256 KB apart: the last ones lie more than 2^32 elements behind the first."""
+    heads, n, stride = (4, 2, 64), 33000, 1 << 17
+    buf = torch.empty(n * stride + stride, dtype=torch.bfloat16, device=DEV)
+    assert n * stride > 1 << 32
+    view = torch.as_strided(buf, (1, n, 2, 64), (buf.numel(), stride, 64, 1))
+    view_v = torch.as_strided(buf, (1, n, 2, 64), (buf.numel(), stride, 64, 1), storage_offset=stride // 2)
+    s = Step(heads, [n - 2], 2, slack=0, seed=17)
+    for mine, far in ((s.k, view), (s.v, view_v)):
+        for lo in range(0, n, 1000):
+            far[:, lo:lo + 1000] = mine[:, lo:lo + 1000]
+    s.k, s.v = view, view_v
+    s.cache = B.make_kv_cache(s.k, s.v)
+    s.run_and_check()
+    # and the eviction moves rows over the same distance
+    weight = torch.arange(n, device=DEV, dtype=torch.float32).reshape(1, n)
+    pos = torch.arange(n, device=DEV, dtype=torch.int32).reshape(1, n)
+    length = torch.tensor([n], dtype=torch.int32, device=DEV)
+    want_k, want_v = s.k[0, n - 3:].clone(), s.v[0, n - 3:].clone()
+    ws = torch.empty(B.lazyllm_op_cache_evict_workspace_bytes(s.cache, 3), dtype=torch.uint8, device=DEV)
+    B.lazyllm_op_cache_evict(s.cache, weight, pos, length, 3, 0, 0, weight, pos, length, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(s.k[0, :3], want_k) and torch.equal(s.v[0, :3], want_v) and pos[0, :3].tolist() == [n - 3, n - 2, n - 1]
+
+
+def test_same_bits_every_time_and_on_another_stream():
+    for prefix in (0, 900):
+        a = Step((32, 8, 128), [1500, 3, 800, -1], 2, prefix=prefix, seed=18)
+        a.run()
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        for _ in range(3):
+            b = Step((32, 8, 128), [1500, 3, 800, -1], 2, prefix=prefix, seed=18)
+            torch.cuda.synchronize()
+            b.run(stream=side)
+            side.synchronize()
+            assert torch.equal(a.o, b.o) and torch.equal(a.weight_out, b.weight_out)
+
+
+@pytest.mark.parametrize("prefix", [0, 300])
+def test_captured_step_replays_as_the_lengths_grow(prefix):
+    """Lengths, positions and inputs live on the device: one captured step serves every later one.  Two graphs share a workspace."""
+    s = Step((4, 2, 64), [100, 0, 257, -1], 1, prefix=prefix, seed=19, max_len=300)
+    eager = Step((4, 2, 64), [100, 0, 257, -1], 1, prefix=prefix, seed=19, max_len=300)
+    s.run()                                                     # (loads the kernels outside the capture)
+    torch.cuda.synchronize()
+    s.weight_out.fill_(-5.0)
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            s.run(stream=torch.cuda.current_stream(), in_place=True)
+        graphs.append(graph)
+    gen = torch.Generator().manual_seed(20)
+    for i in range(6):
+        for x in ("q", "k_new", "v_new"):
+            fresh = torch.randn(getattr(s, x).shape, generator=gen).to(torch.bfloat16).to(DEV)
+            getattr(s, x).copy_(fresh)
+            getattr(eager, x).copy_(fresh)
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        k, v, w = eager.k.clone(), eager.v.clone(), eager.weight.clone()
+        eager.run(in_place=True)
+        torch.cuda.synchronize()
+        assert torch.equal(s.o, eager.o)
+        for b, n in enumerate(eager.lengths):
+            if n >= 0:
+                assert torch.equal(s.weight[b, :n + 1], eager.weight[b, :n + 1]) and torch.equal(s.k[b, :n + 1], eager.k[b, :n + 1])
+        eager.pos[:, :] = -7
+        for b, n in enumerate(eager.lengths):
+            if n >= 0:
+                eager.pos[b, n] = eager.pos_new[b]
+        eager.check(k, v, w, eager.weight)
+        for t in (s, eager):
+            t.len_dev += (t.len_dev >= 0).int()
+            t.pos_new += 1
+        eager.lengths = [n + 1 if n >= 0 else n for n in eager.lengths]
+        eager.pos.fill_(-7)
+
+
+# ---------------------------------------------------------------------------------- eviction
+
+def _evict_expected(weight, pos, n, budget, sinks, recent):
+    """(source slot of every kept slot) by the definition: a sort of the tokens."""
+    if n <= budget:
+        return list(range(max(n, 0)))
+    end = int(pos[:n].max()) + 1
+    rank = []
+    for i in range(n):
+        w = float(weight[i])
+        safe = pos[i] < sinks or pos[i] >= end - recent
+        rank.append((0 if safe else 1, 0.0 if safe else math.inf if math.isnan(w) else -w, 1 if math.isnan(w) and not safe else 0, i))
+    stay = sorted(i for *_, i in sorted(rank)[:budget])
+    movers = [i for i in stay if i >= budget]
+    there = set(stay)
+    return [i if i in there else movers.pop(0) for i in range(budget)]
+
+
+class Cache:
+    def __init__(self, lengths, capacity, heads=(2, 64), seed=0, values="tied", interleaved=False):
+        g = torch.Generator().manual_seed(seed)
+        batch, (kvh, hd) = len(lengths), heads
+        self.lengths, self.capacity = lengths, capacity
+        kv = torch.randn((batch, capacity, 2, kvh, hd), generator=g).to(torch.bfloat16).to(DEV)
+        self.k, self.v = (kv[:, :, 0], kv[:, :, 1]) if interleaved else (kv[:, :, 0].contiguous(), kv[:, :, 1].contiguous())
+        if values == "tied":
+            w = torch.randint(0, 6, (batch, capacity), generator=g).float() / 4
+        elif values == "equal":
+            w = torch.zeros(batch, capacity)
+            w[:, ::3] = -0.0
+        elif values == "odd":
+            w = torch.randn((batch, capacity), generator=g)
+            kind = torch.randint(0, 12, (batch, capacity), generator=g)
+            for code, x in ((0, NAN), (1, math.inf), (2, -math.inf), (3, 0.0), (4, -0.0), (5, 1e-42), (6, 3e38)):
+                w[kind == code] = x
+            w[kind == 7] = -w[kind == 7].abs()
+        else:
+            w = torch.exp(3 * torch.randn((batch, capacity), generator=g)) / capacity
+        self.weight = w.to(DEV)
+        self.pos = (torch.randint(1, 4, (batch, capacity), generator=g).cumsum(1) - 1).to(torch.int32)
+        for b in range(batch):                                 # slots need not be in order of position
+            n = max(0, min(lengths[b], capacity))
+            self.pos[b, :n] = self.pos[b, torch.randperm(n, generator=g)]
+        self.pos = self.pos.to(DEV)
+        self.len_dev = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+        self.cache = B.make_kv_cache(self.k, self.v)
+
+    def run_and_check(self, budget, sinks, recent, in_place=False, stream=None):
+        batch = len(self.lengths)
+        k, v, w, p = self.k.clone(), self.v.clone(), self.weight.clone(), self.pos.clone()
+        wo, po, lo = (self.weight, self.pos, self.len_dev) if in_place else (torch.full_like(w, -3.0), torch.full_like(p, -9), torch.full_like(self.len_dev, -9))
+        kept = torch.full((batch, budget), -2, dtype=torch.int32, device=DEV)
+        ws = torch.full((B.lazyllm_op_cache_evict_workspace_bytes(self.cache, budget),), 255, dtype=torch.uint8, device=DEV)
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        torch.cuda.synchronize()
+        B.lazyllm_op_cache_evict(self.cache, self.weight, self.pos, self.len_dev, budget, sinks, recent, wo, po, lo, ws, kept=kept,
+                                 status=status, stream=stream)
+        torch.cuda.synchronize()
+        assert int(status) == (B.LAZYLLM_ST_BAD_CU if max(self.lengths) > self.capacity else 0)
+        wc, pc = w.cpu().numpy(), p.cpu().numpy()
+        for b, n in enumerate(self.lengths):
+            n = min(n, self.capacity)
+            source = _evict_expected(wc[b], pc[b], n, budget, sinks, recent)
+            m = len(source)
+            assert int(lo[b]) == (min(n, budget) if n >= 0 else n)
+            assert kept[b, :m].tolist() == source and bool((kept[b, m:] == -2).all())
+            at = torch.tensor(source, dtype=torch.long, device=DEV)
+            assert torch.equal(po[b, :m], p[b, at]) and torch.equal(wo[b, :m].view(torch.int32), w[b, at].view(torch.int32))
+            assert torch.equal(self.k[b, :m], k[b, at]) and torch.equal(self.v[b, :m], v[b, at])
+            assert torch.equal(self.k[b, m:], k[b, m:]) and torch.equal(self.v[b, m:], v[b, m:])   # what lies behind is left
+            if in_place:
+                assert torch.equal(po[b, m:], p[b, m:]) and torch.equal(wo[b, m:].view(torch.int32), w[b, m:].view(torch.int32))
+            else:
+                assert bool((po[b, m:] == -9).all()) and bool((wo[b, m:] == -3.0).all())
+
+
+@pytest.mark.parametrize("values", ["tied", "equal", "odd", "spread"])
+@pytest.mark.parametrize("budget,sinks,recent", [(1, 0, 0), (1, 1, 0), (1, 0, 1), (5, 2, 3), (64, 4, 8), (100, 0, 100), (129, 9, 20), (256, 0, 0)])
+def test_eviction_keeps_the_best(values, budget, sinks, recent):
+    Cache([0, 1, -1, 5, 63, 64, 65, 100, 129, 255, 257, 300], 300, seed=budget, values=values).run_and_check(budget, sinks, recent)
+
+
+@pytest.mark.parametrize("values", ["tied", "odd"])
+def test_eviction_in_place(values):
+    c = Cache([300, 12, 0, -3, 301], 301, seed=2, values=values)
+    c.run_and_check(70, 3, 9, in_place=True)
+
+
+@pytest.mark.parametrize("n,budget", [(1, 1), (2, 1), (1024, 1023), (1025, 1024), (2049, 2048), (5000, 4999), (9000, 1000), (70001, 69000), (70000, 33)])
+def test_eviction_of_one_request(n, budget):
+    for values in ("spread", "tied"):
+        Cache([n], n, seed=n, values=values).run_and_check(budget, min(2, budget // 2), budget // 3)
+
+
+def test_eviction_over_many_words():
+    """More 64-slot words than a workgroup has threads."""
+    Cache([200000], 200000, heads=(1, 64), seed=6, values="spread").run_and_check(150000, 4, 1000)
+    Cache([131077, 131000], 131077, heads=(1, 64), seed=7, values="equal").run_and_check(70000, 4, 1000)
+
+
+def test_eviction_with_a_budget_beyond_the_capacity():
+    Cache([100, 40], 100, seed=1).run_and_check(101, 0, 0)
+    Cache([100, 40], 100, seed=1).run_and_check(100, 0, 0)
+
+
+def test_eviction_of_wide_and_interleaved_rows_on_another_stream():
+    side = torch.cuda.Stream()
+    Cache([500, 420], 500, heads=(32, 128), seed=3, values="spread").run_and_check(333, 4, 50, stream=side)
+    Cache([500, 420], 500, heads=(8, 128), seed=3, values="spread", interleaved=True).run_and_check(333, 4, 50)
+
+
+def test_eviction_of_a_length_above_the_capacity():
+    Cache([90, 70], 80, seed=4).run_and_check(50, 1, 2)
+
+
+def test_more_protected_tokens_than_the_budget():
+    """Positions that occur more than once can protect too many: lower slots stay."""
+    c = Cache([50], 50, seed=5)
+    c.pos[:] = 1
+    c.run_and_check(10, 0, 10)
+
+
+def test_captured_eviction_replays():
+    c = Cache([300, 200], 300, seed=8, values="spread")
+    ws = torch.empty(B.lazyllm_op_cache_evict_workspace_bytes(c.cache, 100), dtype=torch.uint8, device=DEV)
+    outs = [torch.zeros_like(c.weight), torch.zeros_like(c.pos), torch.zeros_like(c.len_dev)]
+    call = lambda stream: B.lazyllm_op_cache_evict(c.cache, c.weight, c.pos, c.len_dev, 100, 2, 10, *outs, ws, stream=stream)  # noqa: E731
+    k0 = c.k.clone()
+    call(None)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(torch.cuda.current_stream())
+    for i in range(4):
+        c.k.copy_(k0)
+        c.weight.copy_(torch.rand(c.weight.shape, generator=torch.Generator().manual_seed(i)))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for b, n in enumerate(c.lengths):
+            source = _evict_expected(c.weight[b].cpu().numpy(), c.pos[b].cpu().numpy(), n, 100, 2, 10)
+            assert outs[1][b, :100].tolist() == c.pos[b, torch.tensor(source, device=DEV)].tolist()
+            assert torch.equal(c.k[b, :100], k0[b, torch.tensor(source, device=DEV)])
+
+
+# ---------------------------------------------------------------------------------- together
+
+def test_generation_of_a_batch_from_bounded_caches_after_a_pruned_prefill():
+    """The caches of a layer start as a packed prefill left them (its kept tokens, their positions and Eq. 1 scores); every
+    step appends, attends, adds the weights and evicts.  Requests end and are idle from then on."""
+    shape = synth.TINY
+    w = synth.make_weights(shape, 1001, "cpu")
+    model = B.Model(shape.as_dict(), {k: ([t.to(DEV) for t in v] if isinstance(v, list) else v.to(DEV)) for k, v in w.items()}, DEV)
+    cu = [0, 300, 365, 365 + 128]
+    ids = torch.from_numpy(synth.make_prompt(cu[-1], shape.vocab, 5)).to(DEV)
+    out = model.prefill(ids, [(2, 700), (3, 500)], cu_seqlens=cu)
+    torch.cuda.synchronize()
+    layer, budget, sinks, recent, steps = 3, 80, 2, 16, 8
+    cut = out.cu_kept(layer).tolist()
+    lengths = [b - a for a, b in zip(cut, cut[1:])]
+    assert max(lengths) > budget > min(lengths)
+    s = Step((4, 4, 64), lengths, 1, seed=30, max_len=max(lengths))
+    for b in range(3):
+        rows = slice(cut[b], cut[b + 1])
+        n = lengths[b]
+        s.k[b, :n], s.v[b, :n] = out.k(layer)[rows], out.v(layer)[rows]
+        s.weight[b, :n], s.pos[b, :n] = out.scores(layer)[rows], out.kept_pos(layer)[rows]
+        s.pos_new[b] = cu[b + 1] - cu[b]
+    gen = torch.Generator().manual_seed(31)
+    ws = torch.empty(B.lazyllm_op_cache_evict_workspace_bytes(s.cache, budget), dtype=torch.uint8, device=DEV)
+    for i in range(steps):
+        for x in (s.q, s.k_new, s.v_new):
+            x.copy_(torch.randn(x.shape, generator=gen).to(torch.bfloat16))
+        if i == 5:
+            s.len_dev[1] = -1
+        s.lengths = s.len_dev.tolist()
+        o, size, add, reach = s.expected()
+        before, k, v, p = s.weight.clone(), s.k.clone(), s.v.clone(), s.pos.clone()
+        # (no synchronisation between the two calls: the eviction follows the attention on the stream)
+        s.run(in_place=True)
+        s.len_dev += (s.len_dev >= 0).int()
+        full = s.weight.clone()
+        B.lazyllm_op_cache_evict(s.cache, s.weight, s.pos, s.len_dev, budget, sinks, recent, s.weight, s.pos, s.len_dev, ws)
+        torch.cuda.synchronize()
+        rel = 2 * 68 * 2.0 ** -24 * max(reach, 1.0) + 2.0 ** -16 + 400 * 2.0 ** -24
+        assert bool(((s.o.double() - o).abs() <= o.abs() * 2.0 ** -8 + size * rel + 1e-30).all())
+        for b, n in enumerate(s.lengths):
+            if n < 0:
+                assert int(s.len_dev[b]) == -1 and not s.o[b].any()
+                continue
+            want = torch.cat([before[b, :n], torch.zeros(1, device=DEV)]).double() + add[b, :n + 1]
+            assert bool(((full[b, :n + 1].double() - want).abs() <= add[b, :n + 1] * rel + want * 2.0 ** -23 + 1e-30).all())
+            k[b, n], v[b, n], p[b, n] = s.k_new[b, 0], s.v_new[b, 0], s.pos_new[b]
+            source = _evict_expected(full[b].cpu().numpy(), p[b].cpu().numpy(), n + 1, budget, sinks, recent)
+            m = len(source)
+            at = torch.tensor(source, device=DEV)
+            assert int(s.len_dev[b]) == m == min(n + 1, budget)
+            assert torch.equal(s.pos[b, :m], p[b, at]) and torch.equal(s.weight[b, :m], full[b, at])
+            assert torch.equal(s.k[b, :m], k[b, at]) and torch.equal(s.v[b, :m], v[b, at])
+            assert int(s.pos_new[b]) in s.pos[b, :m].tolist()                # the newest token is protected
+        s.pos_new += 1
+    model.close()

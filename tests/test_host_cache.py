@@ -1,0 +1,119 @@
+"""The entry points over a batch's K,V caches refuse bad arguments on the host, before any HIP call (no GPU here)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2407_14057_amd import binding as B
+
+ONE = 4096                       # an aligned address that is never followed
+
+
+def _cache(**change):
+    c = dict(k=ONE, v=ONE, batch_stride=1000 * 128, row_stride=128, batch=3, capacity=1000, n_kv_heads=2, head_dim=64)
+    c.update(change)
+    return B.lazyllm_kv_cache(**c)
+
+
+def _step(**change):
+    s = dict(q=ONE, k_new=ONE, v_new=ONE, o=ONE, lengths=ONE, n_heads=4, q_len=2, max_len=900, prefix_len=100, prefix_k=ONE,
+             prefix_v=ONE, prefix_stride=128)
+    s.update(change)
+    return B.lazyllm_step_attention(**s)
+
+
+BAD_CACHES = [dict(head_dim=96), dict(head_dim=32), dict(n_kv_heads=0), dict(n_kv_heads=257), dict(batch=0), dict(batch=-1), dict(capacity=0),
+              dict(batch=65536), dict(batch=60000, capacity=60000)]
+BAD_ROWS = [dict(k=0), dict(v=0), dict(k=ONE + 8), dict(v=ONE + 2), dict(row_stride=120), dict(row_stride=132), dict(row_stride=(1 << 24) + 8),
+            dict(row_stride=0), dict(row_stride=-128), dict(batch_stride=1000 * 128 - 8), dict(batch_stride=1000 * 128 + 4), dict(batch_stride=0),
+            dict(batch_stride=-1000 * 128), dict(batch_stride=1 << 50)]
+BAD_STEPS = [dict(n_heads=0), dict(n_heads=3), dict(n_heads=258), dict(q_len=0), dict(q_len=65), dict(max_len=-1), dict(max_len=999),
+             dict(max_len=0x7fffffff)]
+BAD_POINTERS = [dict(q=0), dict(k_new=0), dict(v_new=0), dict(o=0), dict(lengths=0), dict(q=ONE + 8), dict(k_new=ONE + 4), dict(v_new=ONE + 2),
+                dict(o=ONE + 8), dict(weight=ONE), dict(weight_out=ONE), dict(pos=ONE), dict(pos_new=ONE)]
+BAD_PREFIXES = [dict(prefix_len=0), dict(prefix_len=-1), dict(prefix_k=0), dict(prefix_v=0), dict(prefix_k=ONE + 8), dict(prefix_v=ONE + 8),
+                dict(prefix_stride=120), dict(prefix_stride=132), dict(prefix_stride=0), dict(prefix_stride=(1 << 24) + 8)]
+
+
+def _attend(name, cache, step, ws=ONE, size=1 << 40):
+    return getattr(B.lib(), name)(cache and C.byref(cache), step and C.byref(step), ws, size, None)
+
+
+@pytest.mark.parametrize("name", ["lazyllm_op_cache_attention", "lazyllm_op_prefix_attention"])
+def test_attention_refuses_bad_arguments(name):
+    assert _attend(name, None, _step()) == B.LAZYLLM_EINVAL
+    assert _attend(name, _cache(), None) == B.LAZYLLM_EINVAL
+    for change in BAD_CACHES + BAD_ROWS:
+        assert _attend(name, _cache(**change), _step()) == B.LAZYLLM_EINVAL, change
+    for change in BAD_STEPS + BAD_POINTERS:
+        assert _attend(name, _cache(), _step(**change)) == B.LAZYLLM_EINVAL, change
+    assert _attend(name, _cache(), _step(), ws=None) == B.LAZYLLM_EINVAL
+    assert _attend(name, _cache(), _step(), ws=ONE + 128) == B.LAZYLLM_EINVAL
+    prefix = 100 if name == "lazyllm_op_prefix_attention" else 0
+    for weights in (False, True):
+        tables = dict(weight=ONE, weight_out=ONE) if weights else {}
+        size = B.lazyllm_op_cache_attention_workspace_bytes(_cache(), 4, 2, 900, prefix, weights)
+        assert size > 0
+        assert _attend(name, _cache(), _step(**tables), size=size // 2) == B.LAZYLLM_ENOSPC
+        assert _attend(name, _cache(), _step(**tables), size=0) == B.LAZYLLM_ENOSPC
+
+
+def test_prefix_attention_refuses_bad_prefixes():
+    for change in BAD_PREFIXES:
+        assert _attend("lazyllm_op_prefix_attention", _cache(), _step(**change)) == B.LAZYLLM_EINVAL, change
+
+
+def test_workspace_of_the_attention():
+    size = B.lazyllm_op_cache_attention_workspace_bytes
+    for change in BAD_CACHES:
+        assert size(_cache(**change), 4, 2, 100) == 0, change
+    for change in BAD_STEPS:
+        s = _step(**change)
+        assert size(_cache(), s.n_heads, s.q_len, s.max_len) == 0, change
+    assert size(_cache(), 4, 2, 100, -1) == 0
+    assert B.lib().lazyllm_op_cache_attention_workspace_bytes(None, 4, 2, 100, 0, 0) == 0
+    assert size(_cache(), 4, 2, 900, 0, True) > size(_cache(), 4, 2, 900) > 0
+    assert size(_cache(), 4, 2, 900, 5000) > size(_cache(), 4, 2, 900)
+    # sizes whose byte counts pass 32 bits
+    long = _cache(batch=64, capacity=131072, batch_stride=1 << 30)
+    assert size(long, 64, 64, 131072 - 64, 0, True) >= 64 * 64 * 64 * 131072 * 4
+
+
+def _evict(cache=None, size=1 << 40, **change):
+    a = dict(weight=ONE, pos=ONE, lengths=ONE, budget=500, sinks=4, recent=100, weight_out=ONE, pos_out=ONE, lengths_out=ONE, kept=None,
+             status=None, workspace=ONE)
+    a.update(change)
+    return B.lib().lazyllm_op_cache_evict(C.byref(cache or _cache()), a["weight"], a["pos"], a["lengths"], a["budget"], a["sinks"], a["recent"],
+                                          a["weight_out"], a["pos_out"], a["lengths_out"], a["kept"], a["status"], a["workspace"], size, None)
+
+
+def test_eviction_refuses_bad_arguments():
+    for change in BAD_CACHES + BAD_ROWS:
+        assert _evict(_cache(**change)) == B.LAZYLLM_EINVAL, change
+    assert _evict(_cache(batch=1, capacity=524289)) == B.LAZYLLM_EINVAL
+    for name in ("weight", "pos", "lengths", "weight_out", "pos_out", "lengths_out", "workspace"):
+        assert _evict(**{name: None}) == B.LAZYLLM_EINVAL, name
+    for change in (dict(budget=0), dict(budget=-1), dict(sinks=-1), dict(recent=-1), dict(sinks=401), dict(budget=3, sinks=2, recent=2),
+                   dict(sinks=0x7fffffff, recent=0x7fffffff), dict(workspace=ONE + 64)):
+        assert _evict(**change) == B.LAZYLLM_EINVAL, change
+    size = B.lazyllm_op_cache_evict_workspace_bytes(_cache(), 500)
+    assert size > 0 and _evict(size=size - 1) == B.LAZYLLM_ENOSPC and _evict(size=0) == B.LAZYLLM_ENOSPC
+    assert B.lazyllm_op_cache_evict_workspace_bytes(_cache(), 0) == 0
+    assert B.lazyllm_op_cache_evict_workspace_bytes(_cache(head_dim=96), 10) == 0
+    assert B.lazyllm_op_cache_evict_workspace_bytes(_cache(batch=1, capacity=524289), 10) == 0
+    assert B.lib().lazyllm_op_cache_evict(None, ONE, ONE, ONE, 5, 0, 0, ONE, ONE, ONE, None, None, ONE, 1 << 30, None) == B.LAZYLLM_EINVAL
+
+
+def test_descriptor_of_caches():
+    k = torch.zeros(3, 20, 2, 64, dtype=torch.bfloat16)
+    c = B.make_kv_cache(k, torch.zeros_like(k))
+    assert (c.batch, c.capacity, c.n_kv_heads, c.head_dim, c.batch_stride, c.row_stride) == (3, 20, 2, 64, 20 * 128, 128)
+    both = torch.zeros(3, 20, 2, 2, 64, dtype=torch.bfloat16)
+    c = B.make_kv_cache(both[:, :, 0], both[:, :, 1])
+    assert (c.batch_stride, c.row_stride, c.v - c.k) == (20 * 256, 256, 256)
+    heads_first = torch.zeros(3, 2, 20, 64, dtype=torch.bfloat16).transpose(1, 2)
+    for bad_k, bad_v in ((k.float(), k.float()), (k, k[:, :10]), (heads_first, heads_first), (k[0], k[0]), (k, both[:, :, 0]),
+                         (k[..., ::2], k[..., ::2])):
+        with pytest.raises(B.LazyLLMError) as e:
+            B.make_kv_cache(bad_k, bad_v)
+        assert e.value.status == B.LAZYLLM_EINVAL
