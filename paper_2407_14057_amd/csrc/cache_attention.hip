@@ -48,7 +48,7 @@ __device__ __forceinline__ uint32_t pack_halves(uint32_t hi, uint32_t lo, bool u
 // P goes into the second product as two bf16 terms (value and remainder): one alone would add an error as large as the
 // rounding of the output itself, and the matrix cores idle here anyway, the kernel is bound by reading K and V.
 template <int HD, int T>
-__global__ void __launch_bounds__(256, T >= 4 ? 1 : 2) cache_attention_kernel(CacheAttentionArgs a) {
+__global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionArgs a) {
   constexpr int KS = HD / 32;          // k-steps of the first product
   constexpr int NT = HD / 16;          // tiles of 16 output dimensions = dimensions a lane holds of a V row
   constexpr int VW = NT / 2;           // dwords of that
@@ -60,17 +60,20 @@ __global__ void __launch_bounds__(256, T >= 4 ? 1 : 2) cache_attention_kernel(Ca
   const int c = lane & 15, g = lane >> 4;
   const int kvd = a.n_kv * HD;
 
+  // The K,V head varies fastest: workgroups are dealt out to the XCDs in turn, so that ranges that a short request does
+  // not have leave all XCDs with less to do (parts fastest: 8 requests of 1 - 8 k tokens 165 us, now 127), and row
+  // blocks of one range share an L2.
   Item it;
   int b = 0;
   {
     int id = blockIdx.x;
-    const int prefix_items = a.prefix_parts * a.n_kv * a.prefix_blocks;
+    const int prefix_items = a.shared_tiles ? 0 : a.prefix_parts * a.n_kv * a.prefix_blocks;
     it.own = id >= prefix_items;
     if (!it.own) {
-      it.part = id / (a.n_kv * a.prefix_blocks);
-      id %= a.n_kv * a.prefix_blocks;
-      it.kvh = id / a.prefix_blocks;
+      it.kvh = id % a.n_kv;
+      id /= a.n_kv;
       it.row0 = id % a.prefix_blocks * 16 * T;
+      it.part = id / a.prefix_blocks;
       it.n_rows = a.batch * a.q_len * a.group;
       it.tok0 = 0;
       it.stride = a.prefix_stride;
@@ -85,12 +88,12 @@ __global__ void __launch_bounds__(256, T >= 4 ? 1 : 2) cache_attention_kernel(Ca
       it.hi = min(it.lo + a.prefix_range, a.prefix_len);
     } else {
       id -= prefix_items;
-      const int part = id % a.own_parts;
-      id /= a.own_parts;
+      it.kvh = id % a.n_kv;
+      id /= a.n_kv;
       it.row0 = id % a.own_blocks * 16 * T;
       id /= a.own_blocks;
-      it.kvh = id % a.n_kv;
-      b = id / a.n_kv;
+      b = id % a.batch;
+      const int part = id / a.batch;
       it.part = a.prefix_parts + part;
       it.n_rows = a.q_len * a.group;
       it.tok0 = b * a.q_len;
@@ -142,50 +145,62 @@ __global__ void __launch_bounds__(256, T >= 4 ? 1 : 2) cache_attention_kernel(Ca
     for (int i = 0; i < NT; ++i) acc[t][i] = {0.f, 0.f, 0.f, 0.f};
   }
 
-  for (int k0 = it.lo + STEP * wave; k0 < it.hi; k0 += STEP * WAVES) {
+  bf16x8_t kf[2][KS];
+  auto row = [&](const uint16_t* base, const uint16_t* behind, int key, bool tail) {
+    if (!tail || key < it.n) return base + key * it.stride;
+    return behind + min(key - it.n, it.n_tail - 1) * it.tail_stride;
+  };
+  auto load_k = [&](int k0) {
     const bool tail = k0 + STEP > it.n;
-    auto row = [&](const uint16_t* base, const uint16_t* behind, int key) {
-      if (!tail || key < it.n) return base + key * it.stride;
-      return behind + min(key - it.n, it.n_tail - 1) * it.tail_stride;
-    };
-    bf16x8_t kf[2][KS];
-    uint32_t vf[8][VW];
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
-      const uint16_t* kp = row(it.k, it.k_tail, k0 + 16 * sub + c) + 8 * g;
+      const uint16_t* kp = row(it.k, it.k_tail, k0 + 16 * sub + c, tail) + 8 * g;
 #pragma unroll
       for (int s = 0; s < KS; ++s) kf[sub][s] = *(const bf16x8_t*)(kp + 32 * s);
     }
+  };
+  int k0 = it.lo + STEP * wave;
+  if (k0 < it.hi) load_k(k0);
+  for (; k0 < it.hi; k0 += STEP * WAVES) {
+    const bool tail = k0 + STEP > it.n;
+    uint32_t vf[8][VW];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint16_t* vp = row(it.v, it.v_tail, k0 + 16 * (j >> 2) + 4 * g + (j & 3)) + NT * c;
+      const uint16_t* vp = row(it.v, it.v_tail, k0 + 16 * (j >> 2) + 4 * g + (j & 3), tail) + NT * c;
       if (VW == 4) *(uint4*)vf[j] = *(const uint4*)vp;
       else *(uint2*)vf[j] = *(const uint2*)vp;
     }
-    uint4 p_hi[T], p_lo[T];
+    float s[T][8];                      // s[t][4 sub + r]: key k0 + 16 sub + 4 g + r, not scaled
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      float z[8];                       // base-2 logits; z[4 sub + r] belongs to key k0 + 16 sub + 4 g + r
+    for (int t = 0; t < T; ++t)
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
         floatx4_t s4 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < KS; ++s) s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[sub][s], qf[t][s], s4, 0, 0, 0);
+        for (int i = 0; i < KS; ++i) s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[sub][i], qf[t][i], s4, 0, 0, 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) z[4 * sub + r] = s4[r] * a.scale_log2e;
+        for (int r = 0; r < 4; ++r) s[t][4 * sub + r] = s4[r];
       }
+    // the next step's K is on its way during the rest of this one
+    __builtin_amdgcn_sched_barrier(0);
+    if (k0 + STEP * WAVES < it.hi) load_k(k0 + STEP * WAVES);
+    __builtin_amdgcn_sched_barrier(0);
+    uint4 p_hi[T], p_lo[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
       if (tail)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (k0 + 16 * (i >> 2) + 4 * g + (i & 3) > last[t]) z[i] = -INFINITY;
+          if (k0 + 16 * (i >> 2) + 4 * g + (i & 3) > last[t]) s[t][i] = -INFINITY;
       if (a.z != nullptr && it.own && it.row0 + 16 * t + c < it.n_rows) {
         float* zp = a.z + out_row[t] * a.z_ld + k0 + 4 * g;
-        *(float4*)zp = make_float4(z[0], z[1], z[2], z[3]);
-        *(float4*)(zp + 16) = make_float4(z[4], z[5], z[6], z[7]);
+        *(float4*)zp = make_float4(s[t][0] * a.scale_log2e, s[t][1] * a.scale_log2e, s[t][2] * a.scale_log2e, s[t][3] * a.scale_log2e);
+        *(float4*)(zp + 16) = make_float4(s[t][4] * a.scale_log2e, s[t][5] * a.scale_log2e, s[t][6] * a.scale_log2e, s[t][7] * a.scale_log2e);
       }
-      float top = z[0];
+      float top = s[t][0];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, s[t][i]);
+      top *= a.scale_log2e;
       // the reference point of the exponentials follows only when a logit exceeds it by 2^8
       if (__any(top > m_run[t] + 8.f)) {
         top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -201,7 +216,7 @@ __global__ void __launch_bounds__(256, T >= 4 ? 1 : 2) cache_attention_kernel(Ca
       float p[8], rest[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(z[i] - m_use);
+        p[i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale_log2e, -m_use));
         l_run[t] += p[i];
       }
       p_hi[t] = pack8(p);
@@ -286,36 +301,80 @@ __global__ void __launch_bounds__(256, T >= 4 ? 1 : 2) cache_attention_kernel(Ca
   }
 }
 
-// Merges the partial results and adds the weights.  The first workgroups take four output rows each, one a wave; the
-// others 256 slots of a request each: every thread one slot, its rows added in order.
+// (maximum, sum) of one row over its parts, by eight consecutive lanes together; every one of them gets the result.
+__device__ __forceinline__ float2 merged_stat(const float2* __restrict__ st, size_t pitch, int parts, int sub) {
+  float m = -INFINITY, l = 0.f;
+  for (int s0 = 0; s0 < parts; s0 += 32) {
+    float2 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int s = s0 + 8 * u + sub;
+      v[u] = s < parts ? st[s * pitch] : make_float2(-INFINITY, 0.f);
+    }
+    const float top = fmaxf(fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)), m);
+    const float at = top == -INFINITY ? 0.f : top;
+    l *= __builtin_amdgcn_exp2f(m - at);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) l += v[u].y * __builtin_amdgcn_exp2f(v[u].x - at);
+    m = top;
+  }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) {
+    const float m2 = __shfl_xor(m, o, 64), l2 = __shfl_xor(l, o, 64);
+    const float top = fmaxf(m, m2), at = top == -INFINITY ? 0.f : top;
+    l = l * __builtin_amdgcn_exp2f(m - at) + l2 * __builtin_amdgcn_exp2f(m2 - at);
+    m = top;
+  }
+  return make_float2(m, l);
+}
+
+// Merges the partial results and adds the weights.  The first workgroups take an output row each (its parts dealt out to
+// the four waves) or, with few parts, one row a wave; the others 256 slots of a request each: every thread one slot, its
+// rows added in order.
 template <int HD>
 __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) {
+  constexpr int E = HD / 64;           // output dimensions of a lane
   __shared__ float2 stats[256];
+  __shared__ float sums[WAVES][HD];
   const int all_rows = a.batch * a.q_len * a.n_heads;
-  const int merge_groups = a.merge != 0 ? (all_rows + 3) / 4 : 0;
-  const int lane = threadIdx.x & 63;
+  const int merge_groups = a.merge == 0 ? 0 : a.merge == 1 ? (all_rows + WAVES - 1) / WAVES : all_rows;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if ((int)blockIdx.x < merge_groups) {
-    const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= all_rows) return;
+    const int row = a.merge == 1 ? blockIdx.x * WAVES + wave : blockIdx.x;
+    const int first = a.merge == 1 ? 0 : wave, step = a.merge == 1 ? 1 : WAVES;
+    if (row >= all_rows) return;       // (of whole waves, and only where no barrier follows)
     const int n = cached_tokens(a, row / (a.q_len * a.n_heads));
     const int parts = n < 0 ? 0 : a.prefix_parts + (n + a.q_len + a.own_range - 1) / a.own_range;
-    float m = -INFINITY, l = 0.f, x[2] = {0.f, 0.f};
-    for (int s = 0; s < parts; ++s) m = fmaxf(m, a.stat[(size_t)s * all_rows + row].x);
-    for (int s = 0; s < parts; ++s) {
-      const float2 st = a.stat[(size_t)s * all_rows + row];
-      const float w = st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - m);
-      l += w * st.y;
-      const float* src = a.part + ((size_t)s * all_rows + row) * HD;
-      if (HD == 128) {
-        const float2 v = *(const float2*)(src + 2 * lane);
-        x[0] += w * v.x;
-        x[1] += w * v.y;
-      } else {
-        x[0] += w * src[lane];
+    const float2* st = a.stat + row;
+    const float2 ml = merged_stat(st, all_rows, parts, lane & 7);
+    float x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = 0.f;
+    const float* src = a.part + (size_t)row * HD + E * lane;
+    for (int s0 = first; s0 < parts; s0 += 4 * step) {
+      float w[4], v[4][E];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int s = min(s0 + u * step, parts - 1);
+        w[u] = s0 + u * step < parts ? __builtin_amdgcn_exp2f(st[(size_t)s * all_rows].x - ml.x) : 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[u][e] = src[(size_t)s * all_rows * HD + e];
       }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] += w[u] * v[u][e];
     }
-    const float inv = parts == 0 ? 0.f : 1.0f / l;
-    if (HD == 128) ((uint32_t*)(a.o + (size_t)row * HD))[lane] = pack_bf16(x[0] * inv, x[1] * inv);
+    if (a.merge != 1) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) sums[wave][E * lane + e] = x[e];
+      __syncthreads();
+      if (wave != 0) return;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = ((sums[0][E * lane + e] + sums[1][E * lane + e]) + sums[2][E * lane + e]) + sums[3][E * lane + e];
+    }
+    const float inv = parts == 0 ? 0.f : 1.0f / ml.y;
+    if (E == 2) ((uint32_t*)(a.o + (size_t)row * HD))[lane] = pack_bf16(x[0] * inv, x[E - 1] * inv);
     else a.o[(size_t)row * HD + lane] = to_bf16(x[0] * inv);
     return;
   }
@@ -326,30 +385,206 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) 
   if (n < 0 || id % chunks * 256 >= n + a.q_len) return;
   const int rows = a.q_len * a.n_heads, row0 = b * rows;
   const int parts = a.prefix_parts + (n + a.q_len + a.own_range - 1) / a.own_range;
+  const float before = slot < n ? a.weight[(size_t)b * a.capacity + slot] : 0.f;
   float sum = 0.f;
   for (int base = 0; base < rows; base += 256) {
     const int count = min(256, rows - base);
     __syncthreads();
-    if ((int)threadIdx.x < count) {
-      const float2* st = a.stat + row0 + base + threadIdx.x;
-      float m = -INFINITY, l = 0.f;
-      for (int s = 0; s < parts; ++s) m = fmaxf(m, st[(size_t)s * all_rows].x);
-      for (int s = 0; s < parts; ++s) {
-        const float2 v = st[(size_t)s * all_rows];
-        l += v.x == -INFINITY ? 0.f : v.y * __builtin_amdgcn_exp2f(v.x - m);
-      }
-      stats[threadIdx.x] = make_float2(m, 1.0f / l);
+    for (int r = threadIdx.x >> 3; r < count; r += 32) {
+      const float2 ml = merged_stat(a.stat + row0 + base + r, all_rows, parts, threadIdx.x & 7);
+      if ((threadIdx.x & 7) == 0) stats[r] = make_float2(ml.x, 1.0f / ml.y);
     }
     __syncthreads();
     if (slot < n + a.q_len) {
       const float* zp = a.z + (size_t)(row0 + base) * a.z_ld + slot;
-      for (int r = 0; r < count; ++r) sum += __builtin_amdgcn_exp2f(zp[(size_t)r * a.z_ld] - stats[r].x) * stats[r].y;
+      int r = 0;
+      for (; r + 8 <= count; r += 8) {
+        float z[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) z[u] = zp[(size_t)(r + u) * a.z_ld];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sum += __builtin_amdgcn_exp2f(z[u] - stats[r + u].x) * stats[r + u].y;
+      }
+      for (; r < count; ++r) sum += __builtin_amdgcn_exp2f(zp[(size_t)r * a.z_ld] - stats[r].x) * stats[r].y;
     }
   }
-  if (slot < n + a.q_len) {
-    const size_t at = (size_t)b * a.capacity + slot;
-    a.weight_out[at] = (slot < n ? a.weight[at] : 0.f) + sum / (float)a.n_heads;
+  if (slot < n + a.q_len) a.weight_out[(size_t)b * a.capacity + slot] = before + sum / (float)a.n_heads;
+}
+
+// ------------------------------------------------------------------------------------------
+// The prefix for many query rows of a K,V head: the matrix cores bound it.  A workgroup is eight waves of 32 query rows
+// of one K,V head; tiles of 64 keys go through LDS, copied three stages deep by global_load_lds, and every wave reads
+// all of a tile.  Products and layout as above, but V's operand comes out of LDS through the transposing read
+// (ds_read_b64_tr_b16: of four keys' 16 dimensions, lane c gets dimension c of the four), so no vector instruction is
+// spent on it.  The sum of the exponentials is one more row tile of the second product (V = 1): it costs the
+// matrix pipe 1/16 and spares the vector unit, the busier one, an addition per probability.  P is rounded to bf16 once
+// here (the remainder term would cost a third of all MFMAs); the sum is taken over the rounded values.
+// The two waves of a SIMD (w and w + 4) get different priorities, so that one is in its products while the other is in
+// its softmax.
+template <int HD>
+__global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttentionArgs a) {
+  constexpr int KS = HD / 32, NT = HD / 16, BN = 64, T = 2, NW = 8;
+  constexpr int CHK = HD / 8;                        // 16-byte chunks of a row
+  constexpr int TILE = BN * HD * 2;                  // bytes of a K or V tile
+  constexpr int STAGE = 2 * TILE, NS = 3;
+  constexpr int COPIES = TILE / 1024 / NW;           // of each tile per wave
+  constexpr int ROWS_PER_COPY = 64 / CHK;
+  extern __shared__ __attribute__((aligned(1024))) char tiles[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  int id = blockIdx.x;
+  const int kvh = id % a.n_kv;
+  id /= a.n_kv;
+  const int row0 = id % a.prefix_blocks * (16 * T * NW) + 16 * T * wave;
+  const int part = id / a.prefix_blocks;
+  const int n_rows = a.batch * a.q_len * a.group;
+  const int lo = part * a.prefix_range, hi = min(lo + a.prefix_range, a.prefix_len);
+  const bool active = row0 < n_rows;
+  const uint16_t* kbase = a.prefix_k + kvh * HD;
+  const uint16_t* vbase = a.prefix_v + kvh * HD;
+  if (wave < 4) __builtin_amdgcn_s_setprio(1);
+  else __builtin_amdgcn_s_setprio(0);
+
+  auto swz = [](int r) { return CHK == 16 ? swz128(r) : swz64(r); };
+  auto issue = [&](int stage, int k0) {
+#pragma unroll
+    for (int u = 0; u < COPIES; ++u) {
+      const int slab = wave * COPIES + u, r = slab * ROWS_PER_COPY + lane / CHK;
+      const long long off = (long long)min(k0 + r, a.prefix_len - 1) * a.prefix_stride + ((lane % CHK) ^ swz(r)) * 8;
+      g2l16(kbase + off, tiles + stage * STAGE + slab * 1024);
+      g2l16(vbase + off, tiles + stage * STAGE + TILE + slab * 1024);
+    }
+  };
+
+  bf16x8_t qf[T][KS];
+  size_t out_row[T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    const int r = min(row0 + 16 * t + c, n_rows - 1);
+    out_row[t] = (size_t)(r / a.group) * a.n_heads + kvh * a.group + r % a.group;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[t][s] = *(const bf16x8_t*)(a.q + out_row[t] * HD + 32 * s + 8 * g);
   }
+  floatx4_t acc[T][NT], sum[T];
+  float m_run[T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    m_run[t] = -INFINITY;
+    sum[t] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NT; ++i) acc[t][i] = {0.f, 0.f, 0.f, 0.f};
+  }
+  // q is here before the first copy starts: waited for inside the loop, it would have every copy waited for
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[t][s]));
+  const uint4 ones4 = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+  const bf16x8_t ones = *(const bf16x8_t*)&ones4;
+
+  const int steps = (hi - lo + BN - 1) / BN;
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (i < steps) issue(i, lo + i * BN);
+  int stage = 0;
+  for (int it = 0; it < steps; ++it) {
+    const int k0 = lo + it * BN;
+    // this step's copies have landed (those of the next one may be under way), and the stage that the copies
+    // issued below overwrite, the previous step's, is no longer read
+    if (it + 1 < steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * COPIES) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if (it + NS - 1 < steps) issue(stage == 0 ? NS - 1 : stage - 1, k0 + (NS - 1) * BN);
+    const char* kt = tiles + stage * STAGE;
+    const char* vt = kt + TILE;
+    stage = stage + 1 == NS ? 0 : stage + 1;
+    if (!active) continue;
+
+    floatx4_t s[T][4];                               // s[t][sub][r]: key k0 + 16 sub + 4 g + r
+#pragma unroll
+    for (int sub = 0; sub < 4; ++sub) {
+#pragma unroll
+      for (int t = 0; t < T; ++t) s[t][sub] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const int r = 16 * sub + c;
+        const bf16x8_t kf = *(const bf16x8_t*)(kt + r * HD * 2 + (((4 * i + g) ^ swz(r)) * 16));
+#pragma unroll
+        for (int t = 0; t < T; ++t) s[t][sub] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][i], s[t][sub], 0, 0, 0);
+      }
+    }
+    if (k0 + BN > a.prefix_len)
+#pragma unroll
+      for (int sub = 0; sub < 4; ++sub)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (k0 + 16 * sub + 4 * g + r >= a.prefix_len)
+#pragma unroll
+            for (int t = 0; t < T; ++t) s[t][sub][r] = -INFINITY;
+    uint4 p[T][2];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      float top = s[t][0][0];
+#pragma unroll
+      for (int sub = 0; sub < 4; ++sub)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, s[t][sub][r]);
+      top *= a.scale_log2e;
+      if (__any(top > m_run[t] + 8.f)) {
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float m_new = fmaxf(m_run[t], top);
+        const float f = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[t] - m_new);
+        m_run[t] = m_new;
+        asm volatile("; raise the running maximum" ::: "memory");
+        sum[t] *= f;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) acc[t][i] *= f;
+      }
+      const float neg_m = m_run[t] == -INFINITY ? 0.f : -m_run[t];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          e[j] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * u + (j >> 2)][j & 3], a.scale_log2e, neg_m));
+        p[t][u] = pack8(e);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, *(const bf16x8_t*)&p[t][u], sum[t], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        typedef short short4_t __attribute__((ext_vector_type(4)));
+        typedef short short8_t __attribute__((ext_vector_type(8)));
+        short4_t half[2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const int r = 32 * u + 16 * w + 4 * g + (c >> 2);
+          const char* at = vt + r * HD * 2 + (((2 * i + ((c >> 1) & 1)) ^ swz(r)) * 16) + (c & 1) * 8;
+          half[w] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)at);
+        }
+        const short8_t both = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+          acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8_t*)&both, *(const bf16x8_t*)&p[t][u], acc[t][i], 0, 0, 0);
+      }
+    }
+  }
+  const size_t all_rows = (size_t)a.batch * a.q_len * a.n_heads;
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+    if (row0 + 16 * t + c < n_rows) {
+      float* dst = a.part + (part * all_rows + out_row[t]) * HD + 4 * g;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) *(float4*)(dst + 16 * i) = make_float4(acc[t][i][0], acc[t][i][1], acc[t][i][2], acc[t][i][3]);
+      if (g == 0) a.stat[part * all_rows + out_row[t]] = make_float2(m_run[t], sum[t][0]);
+    }
 }
 
 // How a call is cut: rows of an item, key ranges and the workspace.
@@ -358,24 +593,26 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
   CacheAttentionPlan p{};
   const int group = n_heads / n_kv;
   const long long own_rows = (long long)q_len * group, prefix_rows = prefix_len > 0 ? own_rows * batch : 0;
-  const long long rows = prefix_rows > own_rows ? prefix_rows : own_rows;
-  p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  p.own_blocks = (int)((own_rows + 16 * p.tiles - 1) / (16 * p.tiles));
-  p.prefix_blocks = (int)((prefix_rows + 16 * p.tiles - 1) / (16 * p.tiles));
-  auto cut = [](long long keys, long long items, int& range, int& parts) {
-    long long want = 1024 / items;
-    if (want < 1) want = 1;
+  p.shared_tiles = prefix_rows >= 192;
+  p.tiles = (p.shared_tiles || prefix_rows < own_rows ? own_rows : prefix_rows) <= 16 ? 1 : 2;
+  const int rows = 16 * p.tiles, shared_rows = p.shared_tiles ? 256 : rows;
+  p.own_blocks = (int)((own_rows + rows - 1) / rows);
+  p.prefix_blocks = (int)((prefix_rows + shared_rows - 1) / shared_rows);
+  auto cut = [](long long keys, long long items, long long groups, long long least, int& range, int& parts) {
+    const long long want = groups > items ? groups / items : 1;
     long long r = (keys + want - 1) / want;
+    if (r < least) r = least;
     r = (r + 127) / 128 * 128;
-    if (r < 256) r = 256;
     range = (int)r;
     parts = (int)((keys + r - 1) / r);
   };
-  cut((long long)max_len + q_len, (long long)batch * n_kv * p.own_blocks, p.own_range, p.own_parts);
-  if (prefix_len > 0) cut(prefix_len, (long long)n_kv * p.prefix_blocks, p.prefix_range, p.prefix_parts);
+  long long least = 48 * (own_rows < rows ? own_rows : rows);
+  if (least < 256) least = 256;
+  cut((long long)max_len + q_len, (long long)batch * n_kv * p.own_blocks, batch == 1 ? 256 : 4096, least, p.own_range, p.own_parts);
+  if (prefix_len > 0) cut(prefix_len, (long long)n_kv * p.prefix_blocks, 256, 512, p.prefix_range, p.prefix_parts);
   const size_t all_rows = (size_t)batch * q_len * n_heads;
   const int parts = p.own_parts + p.prefix_parts;
-  p.merge = parts > 1;
+  p.merge = parts == 1 ? 0 : parts <= 16 ? 1 : 2;
   p.z_ld = (max_len + q_len + STEP - 1) / STEP * STEP;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   p.part_bytes = p.merge ? up(all_rows * parts * head_dim * 4) : 0;
@@ -389,40 +626,57 @@ hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan
   a.scale_log2e = 1.4426950408889634f / sqrtf((float)head_dim);
   a.own_blocks = p.own_blocks; a.own_range = p.own_range; a.own_parts = p.own_parts;
   a.prefix_blocks = p.prefix_blocks; a.prefix_range = p.prefix_range; a.prefix_parts = p.prefix_parts;
+  a.shared_tiles = p.shared_tiles;
   a.merge = p.merge;
   a.z_ld = p.z_ld;
   char* ws = (char*)workspace;
   a.part = p.part_bytes ? (float*)ws : nullptr;
   a.stat = p.stat_bytes ? (float2*)(ws + p.part_bytes) : nullptr;
   a.z = p.z_bytes ? (float*)(ws + p.part_bytes + p.stat_bytes) : nullptr;
-  const long long items = (long long)p.prefix_parts * a.n_kv * p.prefix_blocks + (long long)a.batch * a.n_kv * p.own_blocks * p.own_parts;
-  if (items > 0x7fffffff) return hipErrorInvalidValue;
+  const long long prefix_items = (long long)p.prefix_parts * a.n_kv * p.prefix_blocks;
+  const long long items = (long long)a.batch * a.n_kv * p.own_blocks * p.own_parts + (p.shared_tiles ? 0 : prefix_items);
+  const long long all_rows = (long long)a.batch * a.q_len * a.n_heads;
+  const long long merge_groups = (a.merge == 0 ? 0 : a.merge == 1 ? (all_rows + WAVES - 1) / WAVES : all_rows) +
+                                 (a.z != nullptr ? (long long)a.batch * ((a.max_len + a.q_len + 255) / 256) : 0);
+  if (prefix_items > 0x7fffffff || items > 0x7fffffff || all_rows > 0x7fffffff || merge_groups > 0x7fffffff)
+    return hipErrorInvalidValue;
+  if (p.shared_tiles) {
+#define LZ_PATT(HD)                                                                                                \
+  do {                                                                                                             \
+    constexpr int LDS_BYTES = 3 * 2 * 64 * HD * 2;                                                                 \
+    auto kern = prefix_attention_kernel<HD>;                                                                       \
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);  \
+    if (e != hipSuccess) return e;                                                                                 \
+    hipLaunchKernelGGL(kern, dim3((unsigned)prefix_items), dim3(512), LDS_BYTES, st, a);                           \
+    e = hipGetLastError();                                                                                         \
+    if (e != hipSuccess) return e;                                                                                 \
+  } while (0)
+    if (head_dim == 128) LZ_PATT(128);
+    else LZ_PATT(64);
+#undef LZ_PATT
+  }
 #define LZ_CATT(HD, T)                                                                                             \
   do {                                                                                                             \
     constexpr int LDS_BYTES = WAVES * 16 * T * (HD + 4) * 4 + WAVES * 16 * T * 8;                                  \
     auto kern = cache_attention_kernel<HD, T>;                                                                     \
-    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);  \
-    if (e != hipSuccess) return e;                                                                                 \
+    if (LDS_BYTES > 65536) {                                                                                       \
+      hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES); \
+      if (e != hipSuccess) return e;                                                                               \
+    }                                                                                                              \
     hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(64 * WAVES), LDS_BYTES, st, a);                           \
   } while (0)
   if (head_dim == 128) {
     if (p.tiles == 1) LZ_CATT(128, 1);
-    else if (p.tiles == 2) LZ_CATT(128, 2);
-    else LZ_CATT(128, 4);
+    else LZ_CATT(128, 2);
   } else {
     if (p.tiles == 1) LZ_CATT(64, 1);
-    else if (p.tiles == 2) LZ_CATT(64, 2);
-    else LZ_CATT(64, 4);
+    else LZ_CATT(64, 2);
   }
 #undef LZ_CATT
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || (a.merge == 0 && a.z == nullptr)) return e;
-  const long long all_rows = (long long)a.batch * a.q_len * a.n_heads;
-  const long long groups = (a.merge != 0 ? (all_rows + 3) / 4 : 0) +
-                           (a.z != nullptr ? (long long)a.batch * ((a.max_len + a.q_len + 255) / 256) : 0);
-  if (all_rows > 0x7fffffff || groups > 0x7fffffff) return hipErrorInvalidValue;
-  if (head_dim == 128) hipLaunchKernelGGL(cache_merge_kernel<128>, dim3((unsigned)groups), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(cache_merge_kernel<64>, dim3((unsigned)groups), dim3(256), 0, st, a);
+  if (e != hipSuccess || merge_groups == 0) return e;
+  if (head_dim == 128) hipLaunchKernelGGL(cache_merge_kernel<128>, dim3((unsigned)merge_groups), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(cache_merge_kernel<64>, dim3((unsigned)merge_groups), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

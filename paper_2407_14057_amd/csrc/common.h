@@ -354,7 +354,7 @@ struct CacheAttentionArgs {
   int32_t* pos;
   int32_t* status;
   // filled in by the launcher
-  int group, own_blocks, own_range, own_parts, prefix_blocks, prefix_range, prefix_parts, merge, z_ld;
+  int group, own_blocks, own_range, own_parts, prefix_blocks, prefix_range, prefix_parts, shared_tiles, merge, z_ld;
   float scale_log2e;
   float* part;                         // [parts][rows][head_dim], rows = batch * q_len * n_heads
   float2* stat;                        // [parts][rows] (maximum, sum), base 2
@@ -362,7 +362,10 @@ struct CacheAttentionArgs {
 };
 struct CacheAttentionPlan {
   int tiles;                           // 16-row tiles of query rows per work item
-  int own_blocks, own_range, own_parts, prefix_blocks, prefix_range, prefix_parts, merge, z_ld;
+  int shared_tiles;                    // the prefix by prefix_attention_kernel
+  int own_blocks, own_range, own_parts, prefix_blocks, prefix_range, prefix_parts;
+  int merge;                           // 0: one part, no merge; else output rows merged by a wave (1) or a workgroup (2) each
+  int z_ld;
   size_t part_bytes, stat_bytes, z_bytes;
   size_t bytes() const { return part_bytes + stat_bytes + z_bytes; }
 };
