@@ -384,7 +384,7 @@ struct EvictArgs {
   float* weight_out;
   int32_t *pos_out, *lengths_out, *kept, *status;
   int32_t* moves;                      // workspace: [batch] counts, then per request holes[max_moves], movers[max_moves]
-  int max_moves;
+  int max_moves, fused;                // fused: the selecting workgroup moves the rows too
 };
 size_t evict_workspace_bytes(int batch, int capacity, int budget);
 hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st);
