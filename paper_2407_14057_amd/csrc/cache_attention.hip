@@ -47,12 +47,15 @@ __device__ __forceinline__ uint32_t pack_halves(uint32_t hi, uint32_t lo, bool u
 //      has dimension HD/16 c + i in row c, and no value of P changes its lane.
 // P goes into the second product as two bf16 terms (value and remainder): one alone would add an error as large as the
 // rounding of the output itself, and the matrix cores idle here anyway, the kernel is bound by reading K and V.
-template <int HD, int T>
+// ONCE: no keys are read by more than one row block.  V then comes by non-temporal loads (8 requests of 1 - 8 k tokens 121
+// -> 113 us, a prefix of 8192 for 16 requests 41 -> 36; K, of whose cache lines a load takes half, loses by them: 124, 38).
+template <int HD, int T, bool ONCE>
 __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionArgs a) {
   constexpr int KS = HD / 32;          // k-steps of the first product
   constexpr int NT = HD / 16;          // tiles of 16 output dimensions = dimensions a lane holds of a V row
   constexpr int VW = NT / 2;           // dwords of that
   constexpr int PITCH = HD + 4;
+  typedef uint32_t words_t __attribute__((ext_vector_type(VW)));
   extern __shared__ __attribute__((aligned(16))) float lds[];   // [WAVES][16 T][PITCH], then float2 [WAVES][16 T]
   float2* ml = (float2*)(lds + WAVES * 16 * T * PITCH);
 
@@ -166,9 +169,8 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
     uint32_t vf[8][VW];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint16_t* vp = row(it.v, it.v_tail, k0 + 16 * (j >> 2) + 4 * g + (j & 3), tail) + NT * c;
-      if (VW == 4) *(uint4*)vf[j] = *(const uint4*)vp;
-      else *(uint2*)vf[j] = *(const uint2*)vp;
+      const words_t* vp = (const words_t*)(row(it.v, it.v_tail, k0 + 16 * (j >> 2) + 4 * g + (j & 3), tail) + NT * c);
+      *(words_t*)vf[j] = ONCE ? __builtin_nontemporal_load(vp) : *vp;
     }
     float s[T][8];                      // s[t][4 sub + r]: key k0 + 16 sub + 4 g + r, not scaled
 #pragma unroll
@@ -329,8 +331,8 @@ __device__ __forceinline__ float2 merged_stat(const float2* __restrict__ st, siz
 }
 
 // Merges the partial results and adds the weights.  The first workgroups take an output row each (its parts dealt out to
-// the four waves) or, with few parts, one row a wave; the others 256 slots of a request each: every thread one slot, its
-// rows added in order.
+// the four waves) or, with few parts, one row a wave; the others 64 slots of a request each: a lane a slot, every wave a
+// quarter of its rows, in a fixed order.
 template <int HD>
 __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) {
   constexpr int E = HD / 64;           // output dimensions of a lane
@@ -379,13 +381,15 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) 
     return;
   }
   const int id = blockIdx.x - merge_groups;
-  const int chunks = (a.max_len + a.q_len + 255) / 256;
-  const int b = id / chunks, slot = id % chunks * 256 + threadIdx.x;
+  const int chunks = (a.max_len + a.q_len + 63) / 64;
+  const int b = id / chunks, slot0 = id % chunks * 64, slot = slot0 + lane;
   const int n = cached_tokens(a, b);
-  if (n < 0 || id % chunks * 256 >= n + a.q_len) return;
+  if (n < 0 || slot0 >= n + a.q_len) return;
   const int rows = a.q_len * a.n_heads, row0 = b * rows;
   const int parts = a.prefix_parts + (n + a.q_len + a.own_range - 1) / a.own_range;
-  const float before = slot < n ? a.weight[(size_t)b * a.capacity + slot] : 0.f;
+  const bool mine = slot < n + a.q_len;
+  const float before = wave == 0 && slot < n ? a.weight[(size_t)b * a.capacity + slot] : 0.f;
+  const float* zp = a.z + (size_t)row0 * a.z_ld + min(slot, n + a.q_len - 1);
   float sum = 0.f;
   for (int base = 0; base < rows; base += 256) {
     const int count = min(256, rows - base);
@@ -395,20 +399,23 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) 
       if ((threadIdx.x & 7) == 0) stats[r] = make_float2(ml.x, 1.0f / ml.y);
     }
     __syncthreads();
-    if (slot < n + a.q_len) {
-      const float* zp = a.z + (size_t)(row0 + base) * a.z_ld + slot;
-      int r = 0;
-      for (; r + 8 <= count; r += 8) {
-        float z[8];
+    // every wave a quarter of the rows
+    const int quarter = (count + WAVES - 1) / WAVES, end = min(count, (wave + 1) * quarter);
+    int r = wave * quarter;
+    for (; r + 8 <= end; r += 8) {
+      float z[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) z[u] = zp[(size_t)(r + u) * a.z_ld];
+      for (int u = 0; u < 8; ++u) z[u] = zp[(size_t)(base + r + u) * a.z_ld];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) sum += __builtin_amdgcn_exp2f(z[u] - stats[r + u].x) * stats[r + u].y;
-      }
-      for (; r < count; ++r) sum += __builtin_amdgcn_exp2f(zp[(size_t)r * a.z_ld] - stats[r].x) * stats[r].y;
+      for (int u = 0; u < 8; ++u) sum += __builtin_amdgcn_exp2f(z[u] - stats[r + u].x) * stats[r + u].y;
     }
+    for (; r < end; ++r) sum += __builtin_amdgcn_exp2f(zp[(size_t)(base + r) * a.z_ld] - stats[r].x) * stats[r].y;
   }
-  if (slot < n + a.q_len) a.weight_out[(size_t)b * a.capacity + slot] = before + sum / (float)a.n_heads;
+  sums[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && mine)
+    a.weight_out[(size_t)b * a.capacity + slot] =
+        before + (((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane]) / (float)a.n_heads;
 }
 
 // ------------------------------------------------------------------------------------------
@@ -587,13 +594,25 @@ __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttention
     }
 }
 
-// How a call is cut: rows of an item, key ranges and the workspace.
+// How a call is cut, measured (us):
+//  - the prefix through shared tiles where its work, query rows of a K,V head x keys x K,V heads x head_dim, is above
+//    2.5 G and there are 128 rows or more: below that the launch more costs more than the tiles save.  In units of 128 M
+//    (rows x keys, 8 K,V heads of 128), direct / shared: 256 x 4000 = 8.2: 23 / 30; 512 x 4000 = 16: 33 / 37;
+//    256 x 16000 = 33: 53 / 46; 1024 x 4000 = 33: 52 / 41; 2048 x 32000: 607 / 272; 32 heads, 64 x 16000 = 33: 76 / 79;
+//    4 heads of 64, 256 x 32000 = 16: 43 / 35, 512 x 4000 = 4: 18 / 24.
+//  - row tiles: one up to 16 rows, else two (a prefix of 3376 for 128 rows: one 21.7, two 18.2, four 22.4).
+//  - ranges of a cache: one request about 256 workgroups (30000 tokens, 8 K,V heads: 34.6 with 256, 38.5 with 512, 44 with
+//    1024), several up to 4096, because their lengths differ (eight of 1 - 8 k: 131 with 1024, 121 with 4096; 64 of up to
+//    2000: 56 / 40), but at least 256 keys and 48 per query row, since a range leaves a partial result of each row
+//    (16 requests of 5 tokens, 20 rows: ranges of 1024 keys 72, of 512 74, of 256 81).
+//  - ranges of the prefix: about 256 workgroups, at least 256 keys per row tile (128 rows, 3376 keys: 256 keys 19.5, 512
+//    18.5; 8 rows of 32 heads, 1000 keys: 20.5 / 22.6).
 CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int head_dim, int q_len, int max_len,
                                         int prefix_len, bool weights) {
   CacheAttentionPlan p{};
   const int group = n_heads / n_kv;
   const long long own_rows = (long long)q_len * group, prefix_rows = prefix_len > 0 ? own_rows * batch : 0;
-  p.shared_tiles = prefix_rows >= 192;
+  p.shared_tiles = prefix_rows >= 128 && (double)prefix_rows * prefix_len * n_kv * head_dim >= 2.5e9;
   p.tiles = (p.shared_tiles || prefix_rows < own_rows ? own_rows : prefix_rows) <= 16 ? 1 : 2;
   const int rows = 16 * p.tiles, shared_rows = p.shared_tiles ? 256 : rows;
   p.own_blocks = (int)((own_rows + rows - 1) / rows);
@@ -609,7 +628,8 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
   long long least = 48 * (own_rows < rows ? own_rows : rows);
   if (least < 256) least = 256;
   cut((long long)max_len + q_len, (long long)batch * n_kv * p.own_blocks, batch == 1 ? 256 : 4096, least, p.own_range, p.own_parts);
-  if (prefix_len > 0) cut(prefix_len, (long long)n_kv * p.prefix_blocks, 256, 512, p.prefix_range, p.prefix_parts);
+  if (prefix_len > 0) cut(prefix_len, (long long)n_kv * p.prefix_blocks, 256, p.shared_tiles ? 256 : 256 * p.tiles, p.prefix_range,
+                          p.prefix_parts);
   const size_t all_rows = (size_t)batch * q_len * n_heads;
   const int parts = p.own_parts + p.prefix_parts;
   p.merge = parts == 1 ? 0 : parts <= 16 ? 1 : 2;
@@ -637,7 +657,7 @@ hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan
   const long long items = (long long)a.batch * a.n_kv * p.own_blocks * p.own_parts + (p.shared_tiles ? 0 : prefix_items);
   const long long all_rows = (long long)a.batch * a.q_len * a.n_heads;
   const long long merge_groups = (a.merge == 0 ? 0 : a.merge == 1 ? (all_rows + WAVES - 1) / WAVES : all_rows) +
-                                 (a.z != nullptr ? (long long)a.batch * ((a.max_len + a.q_len + 255) / 256) : 0);
+                                 (a.z != nullptr ? (long long)a.batch * ((a.max_len + a.q_len + 63) / 64) : 0);
   if (prefix_items > 0x7fffffff || items > 0x7fffffff || all_rows > 0x7fffffff || merge_groups > 0x7fffffff)
     return hipErrorInvalidValue;
   if (p.shared_tiles) {
@@ -655,10 +675,11 @@ hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan
     else LZ_PATT(64);
 #undef LZ_PATT
   }
-#define LZ_CATT(HD, T)                                                                                             \
+  const bool once = p.own_blocks == 1 && (p.shared_tiles || p.prefix_blocks <= 1);
+#define LZ_CATT(HD, T, ONCE)                                                                                             \
   do {                                                                                                             \
     constexpr int LDS_BYTES = WAVES * 16 * T * (HD + 4) * 4 + WAVES * 16 * T * 8;                                  \
-    auto kern = cache_attention_kernel<HD, T>;                                                                     \
+    auto kern = cache_attention_kernel<HD, T, ONCE>;                                                                  \
     if (LDS_BYTES > 65536) {                                                                                       \
       hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES); \
       if (e != hipSuccess) return e;                                                                               \
@@ -666,11 +687,13 @@ hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan
     hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(64 * WAVES), LDS_BYTES, st, a);                           \
   } while (0)
   if (head_dim == 128) {
-    if (p.tiles == 1) LZ_CATT(128, 1);
-    else LZ_CATT(128, 2);
+    if (p.tiles == 1) LZ_CATT(128, 1, true);
+    else if (once) LZ_CATT(128, 2, true);
+    else LZ_CATT(128, 2, false);
   } else {
-    if (p.tiles == 1) LZ_CATT(64, 1);
-    else LZ_CATT(64, 2);
+    if (p.tiles == 1) LZ_CATT(64, 1, true);
+    else if (once) LZ_CATT(64, 2, true);
+    else LZ_CATT(64, 2, false);
   }
 #undef LZ_CATT
   hipError_t e = hipGetLastError();

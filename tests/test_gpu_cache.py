@@ -59,6 +59,10 @@ class Step:
         else:
             B.lazyllm_op_cache_attention(self.cache, *args, **more)
 
+    def shared_tiles(self):
+        rows = self.batch * self.q_len * self.H // self.kvh
+        return self.prefix > 0 and rows >= 128 and rows * self.prefix * self.kvh * self.hd >= 2.5e9
+
     def expected(self):
         """(o, sum of p |v|, added weights per slot [batch, capacity], largest sum of |q_i k_i| / sqrt(hd)) in 64 bits."""
         group = self.H // self.kvh
@@ -90,9 +94,9 @@ class Step:
         # exponential, and the two bf16 terms that it goes into the second product as; sums of up to n terms
         keys = self.prefix + self.max_len + self.q_len
         rel = 2 * (self.hd + 4) * 2.0 ** -24 * max(reach, 1.0) + 2.0 ** -16 + keys * 2.0 ** -24
-        # from 192 query rows of a K,V head on, a probability against the prefix is ONE bf16 term: off by at most 2^-8 of
-        # itself, in the product with V and in the sum that divides it
-        once = 2 * 2.0 ** -8 if self.prefix and self.batch * self.q_len * self.H // self.kvh >= 192 else 0.0
+        # for many query rows a probability against the prefix is ONE bf16 term: off by at most 2^-8 of itself, in the
+        # product with V and in the sum that divides it
+        once = 2 * 2.0 ** -8 if self.shared_tiles() else 0.0
         err = (self.o.double() - o).abs()
         bound = o.abs() * 2.0 ** -8 + size * (rel + once) + 1e-30
         assert bool((err <= bound).all()), (float((err / bound).max()), rel)
@@ -182,12 +186,21 @@ def test_long_shared_prefix():
     Step((32, 8, 128), [3, 0, 700], 1, prefix=20003, seed=10).run_and_check()
 
 
-@pytest.mark.parametrize("heads", ["4x64", "8/1x128"])
-@pytest.mark.parametrize("prefix", [1, 63, 64, 65, 500, 513, 1300, 8000])
-def test_shared_prefix_of_many_rows(heads, prefix):
-    """Many query rows of a K,V head, some requests idle: the last block of rows is not full, nor the last tile of keys."""
+@pytest.mark.parametrize("heads,rows,prefix", [("8/1x128", 8, 128 * 74), ("8/1x128", 8, 9665), ("8/1x128", 8, 9727), ("8/1x128", 8, 10001), ("4x64", 1, 38017),
+                                               ("4x64", 1, 39999), ("32/8x128", 4, 9600), ("4/2x64", 2, 38081)])
+def test_shared_prefix_of_many_rows(heads, rows, prefix):
+    """Many query rows of a K,V head, some requests idle: neither the last block of rows nor the last tile of keys is full."""
     rng = np.random.default_rng(prefix)
-    Step(HEADS[heads], [int(x) for x in rng.integers(-1, 40, 67)], 4, prefix=prefix, seed=prefix).run_and_check()
+    s = Step(HEADS[heads], [int(x) for x in rng.integers(-1, 40, 67)], 4, prefix=prefix, seed=prefix)
+    assert s.H // s.kvh == rows and s.shared_tiles()
+    s.run_and_check()
+
+
+def test_shared_prefix_of_few_keys_and_very_many_rows():
+    """65 keys for 32 tokens of 64 heads on one of 300 requests each: a tile and a key."""
+    s = Step((64, 1, 128), [2] * 300, 32, prefix=65, seed=3, weights=False)
+    assert s.shared_tiles()
+    s.run_and_check()
 
 
 @pytest.mark.parametrize("prefix", [0, 200])
@@ -197,13 +210,14 @@ def test_strided_caches(prefix):
 
 
 def test_strided_prefix():
-    strided = Step((4, 2, 64), [10] * 100, 1, prefix=333, seed=12)
-    for s in (Step((4, 2, 64), [10, 100], 1, prefix=333, seed=12), strided):
-        _stride_prefix(s).run_and_check()
+    _stride_prefix(Step((4, 2, 64), [10, 100], 1, prefix=333, seed=12)).run_and_check()
+    s = _stride_prefix(Step((4, 2, 64), [10] * 100, 2, prefix=49000, seed=12))
+    assert s.shared_tiles()
+    s.run_and_check()
 
 
 def _stride_prefix(s):
-    both = torch.full((333, 3, 2, 64), NAN, dtype=torch.bfloat16, device=DEV)
+    both = torch.full((s.prefix, 3, 2, 64), NAN, dtype=torch.bfloat16, device=DEV)
     both[:, 0], both[:, 2] = s.pk, s.pv
     s.pk, s.pv = both[:, 0], both[:, 2]
     return s
@@ -217,9 +231,10 @@ def test_steep_logits():
     s.run_and_check()
     s = Step((4, 4, 64), [1000, 700], 2, seed=14, spread=20.0)
     s.run_and_check()
-    for batch in (2, 30):
-        s = Step((32, 8, 128), [300, 40] + [7] * (batch - 2), 2, prefix=500, seed=15, spread=20.0)
-        s.pk[400:] *= 2                                       # the maximum moves late
+    for batch, prefix in ((2, 500), (70, 4700)):
+        s = Step((32, 8, 128), [300, 40] + [7] * (batch - 2), 2, prefix=prefix, seed=15, spread=20.0)
+        assert s.shared_tiles() == (batch == 70)
+        s.pk[prefix - 100:] *= 2                              # the maximum moves late
         s.run_and_check()
 
 
