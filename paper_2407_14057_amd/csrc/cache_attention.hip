@@ -11,6 +11,7 @@
 // The partial results (output, maximum, sum) of the ranges are merged by a second launch.
 #include "common.h"
 
+
 namespace lz {
 
 namespace {
@@ -31,6 +32,16 @@ struct Item {
 
 __device__ __forceinline__ int cached_tokens(const CacheAttentionArgs& a, int b) {
   return min(a.lengths[b], a.max_len);            // negative: the request takes no part
+}
+
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef short short8_t __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+// Of four rows' 16 elements, read by 16 lanes 8 bytes each (four lanes a row), lane c gets element c of the four.  The
+// restrict says that no copy into LDS under way writes here: without it the compiler waits for all of them.
+__device__ __forceinline__ short4_t read_transposed(__attribute__((address_space(3))) short4_t* __restrict__ p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
 }
 
 __device__ __forceinline__ uint32_t pack_halves(uint32_t hi, uint32_t lo, bool upper) {
@@ -426,8 +437,10 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) 
 // spent on it.  The sum of the exponentials is one more row tile of the second product (V = 1): it costs the
 // matrix pipe 1/16 and spares the vector unit, the busier one, an addition per probability.  P is rounded to bf16 once
 // here (the remainder term would cost a third of all MFMAs); the sum is taken over the rounded values.
-// The two waves of a SIMD (w and w + 4) get different priorities, so that one is in its products while the other is in
-// its softmax.
+// What bounds it: a step takes 4.0 k cycles of a SIMD, 2.2 k of them the matrix pipe, 2 k vector instructions, while the CU's LDS
+// moves 288 KB; without the LDS reads it would take 3.0 k, without the copies 3.4 k.  Kept in opposite phases by two
+// barriers a step, or with the next scores under the exponentials, the two waves of a SIMD were no faster (300, 280 us
+// where this takes 268: 2048 rows of 8 K,V heads, 32768 keys); nor were three row tiles a wave (314).
 template <int HD>
 __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttentionArgs a) {
   constexpr int KS = HD / 32, NT = HD / 16, BN = 64, T = 2, NW = 8;
@@ -446,22 +459,49 @@ __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttention
   const int part = id / a.prefix_blocks;
   const int n_rows = a.batch * a.q_len * a.group;
   const int lo = part * a.prefix_range, hi = min(lo + a.prefix_range, a.prefix_len);
-  const bool active = row0 < n_rows;
   const uint16_t* kbase = a.prefix_k + kvh * HD;
   const uint16_t* vbase = a.prefix_v + kvh * HD;
-  if (wave < 4) __builtin_amdgcn_s_setprio(1);
-  else __builtin_amdgcn_s_setprio(0);
 
-  auto swz = [](int r) { return CHK == 16 ? swz128(r) : swz64(r); };
+  // Chunk ch of row r lies at chunk ch ^ swizzle(r).  K is read 16 rows x 16 bytes at a time: 16 rows take 16 different
+  // 16-byte units of a 256-byte line; V 8 rows x 32 bytes: eight rows take eight different 32-byte units.
+  auto swz_k = [](int r) { return CHK == 16 ? swz128(r) : swz64(r); };
+  auto swz_v = [](int r) { return CHK == 16 ? (r & 7) << 1 : (r >> 1 & 3) << 1; };
+  // copies of a wave: rows r0 + u * ROWS_PER_COPY of a tile, as byte offsets from the tile's first row
+  const int r0 = wave * COPIES * ROWS_PER_COPY + lane / CHK;
+  uint32_t k_from[COPIES], v_from[COPIES];
+#pragma unroll
+  for (int u = 0; u < COPIES; ++u) {
+    const int r = r0 + u * ROWS_PER_COPY;
+    const uint32_t row = (uint32_t)r * (uint32_t)a.prefix_stride * 2u;
+    k_from[u] = row + ((lane % CHK) ^ swz_k(r)) * 16;
+    v_from[u] = row + ((lane % CHK) ^ swz_v(r)) * 16;
+  }
   auto issue = [&](int stage, int k0) {
+    char* to = tiles + stage * STAGE + wave * COPIES * 1024;
+    const long long row = (long long)k0 * a.prefix_stride;
+    const int last_row = a.prefix_len - 1 - k0;          // rows behind it: the last one again
 #pragma unroll
     for (int u = 0; u < COPIES; ++u) {
-      const int slab = wave * COPIES + u, r = slab * ROWS_PER_COPY + lane / CHK;
-      const long long off = (long long)min(k0 + r, a.prefix_len - 1) * a.prefix_stride + ((lane % CHK) ^ swz(r)) * 8;
-      g2l16(kbase + off, tiles + stage * STAGE + slab * 1024);
-      g2l16(vbase + off, tiles + stage * STAGE + TILE + slab * 1024);
+      uint32_t kf = k_from[u], vf = v_from[u];
+      if (last_row < BN - 1) {
+        const int r = r0 + u * ROWS_PER_COPY;
+        const uint32_t back = (uint32_t)max(r - last_row, 0) * (uint32_t)a.prefix_stride * 2u;
+        kf -= back;
+        vf -= back;
+      }
+      g2l16((const char*)(kbase + row) + kf, to + u * 1024);
+      g2l16((const char*)(vbase + row) + vf, to + TILE + u * 1024);
     }
   };
+  // byte offsets of this lane's operand reads in a stage; 16 rows further on: 32 HD bytes
+  uint32_t k_at[KS], v_at[NT];
+#pragma unroll
+  for (int i = 0; i < KS; ++i) k_at[i] = c * HD * 2 + (((4 * i + g) ^ swz_k(c)) * 16);
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int r = 4 * g + (c >> 2);
+    v_at[i] = TILE + r * HD * 2 + (((2 * i + (c >> 1 & 1)) ^ swz_v(r)) * 16) + (c & 1) * 8;
+  }
 
   bf16x8_t qf[T][KS];
   size_t out_row[T];
@@ -504,24 +544,34 @@ __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttention
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     if (it + NS - 1 < steps) issue(stage == 0 ? NS - 1 : stage - 1, k0 + (NS - 1) * BN);
-    const char* kt = tiles + stage * STAGE;
-    const char* vt = kt + TILE;
+    lds_char* st = (lds_char*)tiles + stage * STAGE;
     stage = stage + 1 == NS ? 0 : stage + 1;
-    if (!active) continue;
 
     floatx4_t s[T][4];                               // s[t][sub][r]: key k0 + 16 sub + 4 g + r
 #pragma unroll
-    for (int sub = 0; sub < 4; ++sub) {
+    for (int sub = 0; sub < 4; ++sub)
 #pragma unroll
       for (int t = 0; t < T; ++t) s[t][sub] = {0.f, 0.f, 0.f, 0.f};
+    // (two key blocks at a time: four accumulators in turn, so that no product waits for the one before it)
 #pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        const int r = 16 * sub + c;
-        const bf16x8_t kf = *(const bf16x8_t*)(kt + r * HD * 2 + (((4 * i + g) ^ swz(r)) * 16));
+    for (int pair = 0; pair < 2; ++pair)
 #pragma unroll
-        for (int t = 0; t < T; ++t) s[t][sub] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][i], s[t][sub], 0, 0, 0);
-      }
+      for (int i = 0; i < KS; ++i)
+#pragma unroll
+        for (int sub = 2 * pair; sub < 2 * pair + 2; ++sub) {
+          const bf16x8_t kf = *(const __attribute__((address_space(3))) bf16x8_t*)(st + k_at[i] + sub * 32 * HD);
+#pragma unroll
+          for (int t = 0; t < T; ++t) s[t][sub] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][i], s[t][sub], 0, 0, 0);
+        }
+    // operand reads run six ahead of the products that take them
+    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+    for (int u = 0; u < 4 * KS - 6; ++u) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
+    __builtin_amdgcn_sched_group_barrier(0x008, 12, 0);
+    __builtin_amdgcn_sched_barrier(0);
     if (k0 + BN > a.prefix_len)
 #pragma unroll
       for (int sub = 0; sub < 4; ++sub)
@@ -567,21 +617,24 @@ __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttention
         sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, *(const bf16x8_t*)&p[t][u], sum[t], 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        typedef short short4_t __attribute__((ext_vector_type(4)));
-        typedef short short8_t __attribute__((ext_vector_type(8)));
         short4_t half[2];
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const int r = 32 * u + 16 * w + 4 * g + (c >> 2);
-          const char* at = vt + r * HD * 2 + (((2 * i + ((c >> 1) & 1)) ^ swz(r)) * 16) + (c & 1) * 8;
-          half[w] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)at);
-        }
+        for (int w = 0; w < 2; ++w)
+          half[w] = read_transposed((__attribute__((address_space(3))) short4_t*)(st + v_at[i] + (2 * u + w) * 32 * HD));
         const short8_t both = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
         for (int t = 0; t < T; ++t)
           acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8_t*)&both, *(const bf16x8_t*)&p[t][u], acc[t][i], 0, 0, 0);
       }
     }
+    __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
+#pragma unroll
+    for (int u = 0; u < 2 * NT - 6; ++u) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 16, 0);
+    __builtin_amdgcn_sched_barrier(0);
   }
   const size_t all_rows = (size_t)a.batch * a.q_len * a.n_heads;
 #pragma unroll
