@@ -599,7 +599,7 @@ int lazyllm_op_prefix_attention(const lazyllm_kv_cache* cache, const lazyllm_ste
  * int32 [batch, capacity] get the tables of the kept tokens (slots 0 .. new length - 1; may be weight and pos
  * themselves), lengths_out int32 [batch] min(length, budget) (may be lengths), and kept, unless NULL, int32
  * [batch, budget], the slot that each slot's token was in.  A negative length stays as it is.  A length above
- * capacity counts as capacity and sets LAZYLLM_ST_BAD_CU in *status (may be NULL).  capacity <= 524288. */
+ * capacity counts as capacity and sets LAZYLLM_ST_BAD_CU in *status (may be NULL).  capacity up to 2^24. */
 size_t lazyllm_op_cache_evict_workspace_bytes(const lazyllm_kv_cache* cache, int32_t budget);
 int lazyllm_op_cache_evict(const lazyllm_kv_cache* cache, const float* weight, const int32_t* pos,
                            const int32_t* lengths, int32_t budget, int32_t sinks, int32_t recent, float* weight_out,

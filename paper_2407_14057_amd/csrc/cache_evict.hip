@@ -49,143 +49,54 @@ __device__ __forceinline__ void count_bins(int* hist, uint32_t bin, bool on) {
   }
 }
 
-}  // namespace
+// The radix select, most significant bits first: 11, 11 and 10 of the key.  (The first 11 bits of a weight are its
+// exponent and two bits more, so that few lanes of a wave meet in a bin; by 8 bits the weights of a prompt fall into
+// five bins.)
+constexpr int PASSES = 3, BINS = 2048;
+__device__ __forceinline__ int pass_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ __forceinline__ int pass_bins(int pass) { return pass == 2 ? 1024 : 2048; }
+__device__ __forceinline__ uint32_t pass_bin(uint32_t key, int pass) { return (key >> pass_shift(pass)) & (uint32_t)(pass_bins(pass) - 1); }
 
-// THREADS threads; ITEMS slots per thread are kept in registers (0: any number, read again from memory where needed).
-// Threshold: MSB-first radix select by 11, 11 and 10 bits, a barrier each: every wave reads the histogram for itself.  (The
-// first 11 bits of a weight are its exponent and two bits more, so that few lanes of a wave meet in a bin; by 8 bits the
-// weights of a prompt fall into five bins.)
-template <int THREADS, int ITEMS>
-__global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
-  constexpr int WAVES = THREADS / 64, BINS = 2048;
-  extern __shared__ __attribute__((aligned(16))) unsigned long long words[];   // keep[W], equal[W]
-  __shared__ __attribute__((aligned(16))) int hist[3][BINS];
-  __shared__ int2 part[WAVES];
-  __shared__ int list[2][FUSED_MOVES];
-  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const float* weight = a.weight + (size_t)b * a.capacity;
-  const int32_t* pos = a.pos + (size_t)b * a.capacity;
-  float* weight_out = a.weight_out + (size_t)b * a.capacity;
-  int32_t* pos_out = a.pos_out + (size_t)b * a.capacity;
-  int32_t* kept_from = a.kept != nullptr ? a.kept + (size_t)b * a.budget : nullptr;
-  const int given = a.lengths[b], n = min(given, a.capacity), kept = min(n, a.budget);
-  for (int i = threadIdx.x; i < 3 * BINS / 4; i += THREADS) ((int4*)hist)[i] = make_int4(0, 0, 0, 0);
+// What a select has found out: the key of rank `need` among those that begin with `prefix` (bits of `mask`), and at the
+// end how many keys equal it.
+struct Found {
+  uint32_t prefix = 0u, mask = 0u;
+  int need = 0, same = 0;
+};
+// Goes on by one pass, given its histogram.  A wave does it for itself; every lane gets the result.  Counted from the top:
+// lane L owns the `per` bins below bins - per * L, then lane l one of the bins of the lane that the rank falls to.
+__device__ __forceinline__ void next_digit(Found& f, const int* hist, int pass) {
+  const int lane = threadIdx.x & 63, bins = pass_bins(pass), per = bins / 64;
+  int mine = 0;
+  for (int u = 0; u < per / 4; ++u) {
+    const int4 h = *(const int4*)&hist[bins - per * (lane + 1) + 4 * ((u + lane) % (per / 4))];   // (staggered over the banks)
+    mine += (h.x + h.y) + (h.z + h.w);
+  }
+  int incl = wave_scan(mine);
+  int at = __builtin_ctzll(__ballot(incl >= f.need));
+  f.need -= __builtin_amdgcn_readlane(incl - mine, at);
+  const int top = bins - per * at - 1;
+  mine = lane < per ? hist[top - lane] : 0;
+  incl = wave_scan(mine);
+  at = __builtin_ctzll(__ballot(incl >= f.need));
+  f.need -= __builtin_amdgcn_readlane(incl - mine, at);
+  f.same = __builtin_amdgcn_readlane(mine, at);
+  f.prefix |= (uint32_t)(top - at) << pass_shift(pass);
+  f.mask |= (uint32_t)(bins - 1) << pass_shift(pass);
+}
 
-  float w[ITEMS > 0 ? ITEMS : 1];
-  int p[ITEMS > 0 ? ITEMS : 1];
-  uint32_t keys[ITEMS > 0 ? ITEMS : 1];
-  int top = INT32_MIN;
-  // calls f(item, slot, weight, position) for this thread's slots below n; all lanes of a wave together where f needs it
-  auto each = [&](auto f) {
-    if (ITEMS > 0) {
-#pragma unroll
-      for (int u = 0; u < ITEMS; ++u)
-        if (u * THREADS < n) f(u, u * THREADS + (int)threadIdx.x, w[u], p[u]);
-    } else {
-      constexpr int AHEAD = 8;             // loads in flight
-      for (int u0 = 0; u0 * THREADS < n; u0 += AHEAD) {
-        float wi[AHEAD];
-        int pi[AHEAD];
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-          const int i = min((u0 + u) * THREADS + (int)threadIdx.x, n - 1);
-          wi[u] = weight[i];
-          pi[u] = pos[i];
-        }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-          if ((u0 + u) * THREADS < n) f(u0 + u, (u0 + u) * THREADS + (int)threadIdx.x, wi[u], pi[u]);
-      }
-    }
-  };
-  if (ITEMS > 0) {
-#pragma unroll
-    for (int u = 0; u < ITEMS; ++u)
-      if (u * THREADS < n) {
-        const int i = u * THREADS + threadIdx.x;
-        w[u] = i < n ? weight[i] : 0.f;
-        p[u] = i < n ? pos[i] : INT32_MIN;
-      }
-  }
-  each([&](int, int i, float, int at) { if (i < n) top = max(top, at); });
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
-  if (lane == 0) part[wave].x = top;
-  __syncthreads();                       // (also: every thread has read the length, which may be overwritten now)
-#pragma unroll
-  for (int v = 0; v < WAVES; ++v) top = max(top, part[v].x);
-  if (threadIdx.x == 0) {
-    a.lengths_out[b] = kept;
-    if (given > a.capacity && a.status != nullptr) atomicOr(a.status, ST_BAD_CU);
-  }
-  const bool new_weight = weight_out != weight, new_pos = pos_out != pos;
-  auto stay = [&](int i, float wi, int pi) {
-    if (new_weight) weight_out[i] = wi;
-    if (new_pos) pos_out[i] = pi;
-    if (kept_from != nullptr) kept_from[i] = i;
-  };
-  if (n <= a.budget) {
-    each([&](int, int i, float wi, int pi) { if (i < kept) stay(i, wi, pi); });
-    if (threadIdx.x == 0 && !a.fused) a.moves[b] = 0;
-    return;
-  }
-  const bool any_recent = a.recent > 0;
-  const int recent_from = (int)max((long long)top + 1 - (any_recent ? a.recent : 1), (long long)INT32_MIN);
-  if (ITEMS > 0)
-    each([&](int u, int i, float wi, int pi) { keys[u] = eviction_key(wi, pi, a.sinks, any_recent, recent_from); });
-  auto key_of = [&](int u, float wi, int pi) {
-    return ITEMS > 0 ? keys[u] : eviction_key(wi, pi, a.sinks, any_recent, recent_from);
-  };
+__device__ __forceinline__ int first_recent(int top, int recent) {
+  return (int)max((long long)top + 1 - (recent > 0 ? recent : 1), (long long)INT32_MIN);
+}
 
-  // the key of rank `kept` from above, and how many of its duplicates are kept
-  uint32_t threshold = 0u, mask = 0u;
-  int need = kept, same = 0;
-#pragma unroll
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-    each([&](int u, int i, float wi, int pi) {
-      const uint32_t key = key_of(u, wi, pi);
-      count_bins(hist[pass], (key >> shift) & (bins - 1), i < n && (key & mask) == threshold);
-    });
-    __syncthreads();
-    // counted from the top: lane L owns the `per` bins below bins - per * L, then lane l one of the bins of the lane
-    // that the rank falls to
-    const int per = bins / 64;
-    int mine = 0;
-#pragma unroll
-    for (int u = 0; u < per / 4; ++u) {
-      const int4 h = *(const int4*)&hist[pass][bins - per * (lane + 1) + 4 * ((u + lane) % (per / 4))];   // (staggered over the banks)
-      mine += (h.x + h.y) + (h.z + h.w);
-    }
-    int incl = wave_scan(mine);
-    int at = __builtin_ctzll(__ballot(incl >= need));
-    need -= __builtin_amdgcn_readlane(incl - mine, at);
-    const int top_bin = bins - per * at - 1;
-    mine = lane < per ? hist[pass][top_bin - lane] : 0;
-    incl = wave_scan(mine);
-    at = __builtin_ctzll(__ballot(incl >= need));
-    need -= __builtin_amdgcn_readlane(incl - mine, at);
-    same = __builtin_amdgcn_readlane(mine, at);
-    threshold |= (uint32_t)(top_bin - at) << shift;
-    mask |= (uint32_t)(bins - 1) << shift;
-  }
-
-  // kept set as a bit mask: keys above the threshold, and the first `need` equal to it
-  const int W = (n + 63) / 64;
-  unsigned long long* keep = words;
-  unsigned long long* equal = words + (a.capacity + 63) / 64;
-  const bool all_equal = need == same;
-  each([&](int u, int i, float wi, int pi) {
-    const uint32_t key = key_of(u, wi, pi);
-    const unsigned long long hi = __ballot(i < n && (all_equal ? key >= threshold : key > threshold));
-    const unsigned long long eq = __ballot(i < n && key == threshold);
-    const int at = u * WAVES + wave;
-    if (lane == 0 && at < W) {
-      keep[at] = hi;
-      equal[at] = eq;
-    }
-  });
-  __syncthreads();
+// From the bit masks of the keys above the threshold (keep) and equal to it: which of the equal ones stay (the first
+// `need`), and the list of moves.  Holes are slots below the budget that lose their token, movers kept tokens from behind
+// it; as many of each, returned.  All threads of the workgroup; keep is complete on return, the lists after a barrier.
+template <int THREADS>
+__device__ __forceinline__ int resolve_moves(unsigned long long* keep, const unsigned long long* equal, int W, int kept, int need,
+                                             bool all_equal, int32_t* hole_at, int32_t* mover_at, int2* part) {
+  constexpr int WAVES = THREADS / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // exclusive sums over the words, a thread a word, of two counts at once; total: of all of them.  Up to 64 words every
   // wave makes for itself.
   auto over_words = [&](int x, int y, int2& total) {
@@ -228,10 +139,6 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
     }
     __syncthreads();
   }
-
-  // moves: holes are slots below the budget that lose their token, movers kept tokens from behind it; as many of each
-  int32_t* hole_at = a.fused ? list[0] : a.moves + a.batch + (size_t)b * 2 * a.max_moves;
-  int32_t* mover_at = a.fused ? list[1] : hole_at + a.max_moves;
   int2 done = make_int2(0, 0);            // holes, movers
   for (int w0 = 0; w0 < W; w0 += stride) {
     const int at = w0 + own;
@@ -248,10 +155,94 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
       for (; mover != 0ull; mover &= mover - 1ull) mover_at[m++] = 64 * at + __builtin_ctzll(mover);
     }
   }
-  const int holes = done.x;
+  return done.x;
+}
+
+}  // namespace
+
+// THREADS threads, ITEMS slots per thread in registers.  Every wave reads the histograms for itself: a barrier a pass.
+template <int THREADS, int ITEMS>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
+  constexpr int WAVES = THREADS / 64;
+  __shared__ unsigned long long keep[THREADS * ITEMS / 64], equal[THREADS * ITEMS / 64];
+  __shared__ __attribute__((aligned(16))) int hist[PASSES][BINS];
+  __shared__ int2 part[WAVES];
+  __shared__ int list[2][FUSED_MOVES];
+  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float* weight = a.weight + (size_t)b * a.capacity;
+  const int32_t* pos = a.pos + (size_t)b * a.capacity;
+  float* weight_out = a.weight_out + (size_t)b * a.capacity;
+  int32_t* pos_out = a.pos_out + (size_t)b * a.capacity;
+  int32_t* kept_from = a.kept != nullptr ? a.kept + (size_t)b * a.budget : nullptr;
+  const int given = a.lengths[b], n = min(given, a.capacity), kept = min(n, a.budget);
+  for (int i = threadIdx.x; i < PASSES * BINS / 4; i += THREADS) ((int4*)hist)[i] = make_int4(0, 0, 0, 0);
+
+  float w[ITEMS];
+  int p[ITEMS];
+  uint32_t keys[ITEMS];
+  // calls f(item, slot) for the items that any thread has a slot below n for; all lanes of a wave together
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u)
+      if (u * THREADS < n) f(u, u * THREADS + (int)threadIdx.x);
+  };
+  each([&](int u, int i) {
+    w[u] = i < n ? weight[i] : 0.f;
+    p[u] = i < n ? pos[i] : INT32_MIN;
+  });
+  int top = INT32_MIN;
+  each([&](int u, int) { top = max(top, p[u]); });
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
+  if (lane == 0) part[wave].x = top;
+  __syncthreads();                       // (also: every thread has read the length, which may be overwritten now)
+#pragma unroll
+  for (int v = 0; v < WAVES; ++v) top = max(top, part[v].x);
+  if (threadIdx.x == 0) {
+    a.lengths_out[b] = kept;
+    if (given > a.capacity && a.status != nullptr) atomicOr(a.status, ST_BAD_CU);
+  }
+  const bool new_weight = weight_out != weight, new_pos = pos_out != pos;
+  auto stay = [&](int u, int i) {
+    if (new_weight) weight_out[i] = w[u];
+    if (new_pos) pos_out[i] = p[u];
+    if (kept_from != nullptr) kept_from[i] = i;
+  };
+  if (n <= a.budget) {
+    each([&](int u, int i) { if (i < kept) stay(u, i); });
+    if (threadIdx.x == 0 && !a.fused) a.moves[b] = 0;
+    return;
+  }
+  const int recent_from = first_recent(top, a.recent);
+  each([&](int u, int) { keys[u] = eviction_key(w[u], p[u], a.sinks, a.recent > 0, recent_from); });
+  Found f;
+  f.need = kept;
+#pragma unroll
+  for (int pass = 0; pass < PASSES; ++pass) {
+    each([&](int u, int i) { count_bins(hist[pass], pass_bin(keys[u], pass), i < n && (keys[u] & f.mask) == f.prefix); });
+    __syncthreads();
+    next_digit(f, hist[pass], pass);
+  }
+
+  // kept set as a bit mask: keys above the threshold, and the first `need` equal to it
+  const int W = (n + 63) / 64;
+  const bool all_equal = f.need == f.same;
+  each([&](int u, int i) {
+    const unsigned long long hi = __ballot(i < n && (all_equal ? keys[u] >= f.prefix : keys[u] > f.prefix));
+    const unsigned long long eq = __ballot(i < n && keys[u] == f.prefix);
+    const int at = u * WAVES + wave;
+    if (lane == 0 && at < W) {
+      keep[at] = hi;
+      equal[at] = eq;
+    }
+  });
+  __syncthreads();
+  int32_t* hole_at = a.fused ? list[0] : a.moves + a.batch + (size_t)b * 2 * a.max_moves;
+  int32_t* mover_at = a.fused ? list[1] : hole_at + a.max_moves;
+  const int holes = resolve_moves<THREADS>(keep, equal, W, kept, f.need, all_equal, hole_at, mover_at, part);
   if (threadIdx.x == 0 && !a.fused) a.moves[b] = holes;
   if (new_weight || new_pos || kept_from != nullptr)
-    each([&](int, int i, float wi, int pi) { if (i < kept && ((keep[i >> 6] >> (i & 63)) & 1ull)) stay(i, wi, pi); });
+    each([&](int u, int i) { if (i < kept && ((keep[i >> 6] >> (i & 63)) & 1ull)) stay(u, i); });
   __syncthreads();                        // the lists are read by other threads of this workgroup
   for (int i = threadIdx.x; i < holes; i += THREADS) {
     const int to = hole_at[i], from = mover_at[i];
@@ -268,6 +259,170 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
     const uint4 x = *(const uint4*)(k + from), y = *(const uint4*)(v + from);
     *(uint4*)(k + to) = x;
     *(uint4*)(v + to) = y;
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// Caches of more slots: a workgroup per SEG slots, a launch per pass (one workgroup for 131000 slots took 176 us, nearly all
+// of it waiting for its own loads and LDS; these launches 35).  Per request the workspace holds the
+// segments' highest positions, the histograms, the bit masks and the new length.
+constexpr int SEG = 8192, SEG_THREADS = 512, SEG_ITEMS = SEG / SEG_THREADS;
+
+namespace {
+
+struct LongState {                       // of one request, in the workspace
+  int32_t *top, *hist, *kept;
+  unsigned long long *keep, *equal;
+};
+__host__ __device__ inline size_t long_state_bytes(int capacity) {
+  const size_t segs = (capacity + SEG - 1) / SEG;
+  return PASSES * BINS * 4 + segs * (SEG / 64) * 16 + ((segs + 1) * 4 + 255) / 256 * 256;
+}
+__device__ __forceinline__ LongState long_state(const EvictArgs& a, int b) {
+  const size_t segs = (a.capacity + SEG - 1) / SEG;
+  char* at = (char*)a.long_state + b * long_state_bytes(a.capacity);
+  LongState s;
+  s.hist = (int32_t*)at;
+  s.keep = (unsigned long long*)(at + PASSES * BINS * 4);
+  s.equal = s.keep + segs * (SEG / 64);
+  s.top = (int32_t*)(s.equal + segs * (SEG / 64));
+  s.kept = s.top + segs;
+  return s;
+}
+// Highest position of a request, from its segments'; all threads of a wave together.
+__device__ __forceinline__ int highest(const LongState& s, int n) {
+  const int lane = threadIdx.x & 63;
+  int top = INT32_MIN;
+  for (int i = lane; i * SEG < n; i += 64) top = max(top, s.top[i]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
+  return top;
+}
+
+}  // namespace
+
+// Highest position of a segment; the histograms are cleared.
+__global__ void __launch_bounds__(SEG_THREADS) evict_long_top_kernel(EvictArgs a) {
+  __shared__ int part[SEG_THREADS / 64];
+  const int b = blockIdx.y, seg = blockIdx.x, n = min(a.lengths[b], a.capacity);
+  const LongState s = long_state(a, b);
+  for (int i = seg * SEG_THREADS + threadIdx.x; i < PASSES * BINS / 4; i += gridDim.x * SEG_THREADS)
+    ((int4*)s.hist)[i] = make_int4(0, 0, 0, 0);
+  const int32_t* pos = a.pos + (size_t)b * a.capacity;
+  int top = INT32_MIN;
+#pragma unroll
+  for (int u = 0; u < SEG_ITEMS; ++u) {
+    const int i = seg * SEG + u * SEG_THREADS + threadIdx.x;
+    top = max(top, i < n ? pos[i] : INT32_MIN);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int v = 1; v < SEG_THREADS / 64; ++v) top = max(top, part[v]);
+    s.top[seg] = top;
+  }
+}
+
+// PASS < PASSES: counts a segment's keys of that pass; PASS == PASSES: writes its bit masks.
+template <int PASS>
+__global__ void __launch_bounds__(SEG_THREADS) evict_long_pass_kernel(EvictArgs a) {
+  __shared__ __attribute__((aligned(16))) int hist[BINS];
+  const int b = blockIdx.y, seg = blockIdx.x, n = min(a.lengths[b], a.capacity);
+  if (n <= a.budget || seg * SEG >= n) return;
+  const LongState s = long_state(a, b);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float* weight = a.weight + (size_t)b * a.capacity;
+  const int32_t* pos = a.pos + (size_t)b * a.capacity;
+  float w[SEG_ITEMS];
+  int p[SEG_ITEMS];
+#pragma unroll
+  for (int u = 0; u < SEG_ITEMS; ++u) {
+    const int i = min(seg * SEG + u * SEG_THREADS + (int)threadIdx.x, n - 1);
+    w[u] = weight[i];
+    p[u] = pos[i];
+  }
+  if (PASS < PASSES) {
+    for (int i = threadIdx.x; i < BINS / 4; i += SEG_THREADS) ((int4*)hist)[i] = make_int4(0, 0, 0, 0);
+    __syncthreads();
+  }
+  const int recent_from = first_recent(highest(s, n), a.recent);
+  Found f;
+  f.need = a.budget;
+#pragma unroll
+  for (int pass = 0; pass < PASS; ++pass) next_digit(f, s.hist + pass * BINS, pass);
+#pragma unroll
+  for (int u = 0; u < SEG_ITEMS; ++u) {
+    const int i = seg * SEG + u * SEG_THREADS + threadIdx.x;
+    const uint32_t key = eviction_key(w[u], p[u], a.sinks, a.recent > 0, recent_from);
+    if (PASS < PASSES) {
+      count_bins(hist, pass_bin(key, PASS), i < n && (key & f.mask) == f.prefix);
+    } else {
+      const unsigned long long hi = __ballot(i < n && (f.need == f.same ? key >= f.prefix : key > f.prefix));
+      const unsigned long long eq = __ballot(i < n && key == f.prefix);
+      if (lane == 0) {
+        const int at = seg * (SEG / 64) + u * (SEG_THREADS / 64) + wave;
+        s.keep[at] = hi;
+        s.equal[at] = eq;
+      }
+    }
+  }
+  if (PASS < PASSES) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < pass_bins(PASS); i += SEG_THREADS)
+      if (hist[i] != 0) atomicAdd(&s.hist[PASS * BINS + i], hist[i]);
+  }
+}
+
+// A request's moves, and its new length.
+__global__ void __launch_bounds__(1024) evict_long_moves_kernel(EvictArgs a) {
+  __shared__ int2 part[16];
+  const int b = blockIdx.x;
+  const LongState s = long_state(a, b);
+  const int given = a.lengths[b], n = min(given, a.capacity), kept = min(n, a.budget);
+  __syncthreads();                       // every thread has read the length, which may be overwritten now
+  int holes = 0;
+  if (n > a.budget) {
+    Found f;
+    f.need = kept;
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) next_digit(f, s.hist + pass * BINS, pass);
+    int32_t* hole_at = a.moves + a.batch + (size_t)b * 2 * a.max_moves;
+    holes = resolve_moves<1024>(s.keep, s.equal, (n + 63) / 64, kept, f.need, f.need == f.same, hole_at, hole_at + a.max_moves, part);
+  }
+  if (threadIdx.x == 0) {
+    a.moves[b] = holes;
+    *s.kept = kept;
+    a.lengths_out[b] = kept;
+    if (given > a.capacity && a.status != nullptr) atomicOr(a.status, ST_BAD_CU);
+  }
+}
+
+// The tables of the kept tokens: of those that stay where they are, unless the table is its own output, and of those that move.
+__global__ void __launch_bounds__(256) evict_long_tables_kernel(EvictArgs a) {
+  const int b = blockIdx.y, threads = gridDim.x * 256, first = blockIdx.x * 256 + threadIdx.x;
+  const LongState s = long_state(a, b);
+  const int kept = *s.kept, holes = a.moves[b];
+  const float* weight = a.weight + (size_t)b * a.capacity;
+  const int32_t* pos = a.pos + (size_t)b * a.capacity;
+  float* weight_out = a.weight_out + (size_t)b * a.capacity;
+  int32_t* pos_out = a.pos_out + (size_t)b * a.capacity;
+  int32_t* kept_from = a.kept != nullptr ? a.kept + (size_t)b * a.budget : nullptr;
+  const bool all_stay = holes == 0;
+  if (weight_out != weight || pos_out != pos || kept_from != nullptr)
+    for (int i = first; i < kept; i += threads)
+      if (all_stay || ((s.keep[i >> 6] >> (i & 63)) & 1ull)) {
+        if (weight_out != weight) weight_out[i] = weight[i];
+        if (pos_out != pos) pos_out[i] = pos[i];
+        if (kept_from != nullptr) kept_from[i] = i;
+      }
+  const int32_t* hole_at = a.moves + a.batch + (size_t)b * 2 * a.max_moves;
+  for (int i = first; i < holes; i += threads) {
+    const int to = hole_at[i], from = hole_at[a.max_moves + i];
+    weight_out[to] = weight[from];
+    pos_out[to] = pos[from];
+    if (kept_from != nullptr) kept_from[to] = from;
   }
 }
 
@@ -288,32 +443,40 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
   }
 }
 
-size_t evict_workspace_bytes(int batch, int capacity, int budget) {
+// The largest capacity that one workgroup selects from: up to here its launch is the quicker one (16000 slots: 28 us, of
+// which 19 are the selection, against some 30 for the launches of the long form).
+constexpr int SELECT_CAPACITY = 16384;
+
+static size_t move_bytes(int batch, int capacity, int budget) {
   const int most = budget < capacity - budget ? budget : capacity - budget;
   return ((size_t)batch * (1 + 2 * (size_t)(most > 0 ? most : 0)) * 4 + 255) & ~(size_t)255;
+}
+
+size_t evict_workspace_bytes(int batch, int capacity, int budget) {
+  return move_bytes(batch, capacity, budget) + (capacity > SELECT_CAPACITY ? (size_t)batch * long_state_bytes(capacity) : 0);
 }
 
 hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st) {
   const int most = a.budget < a.capacity - a.budget ? a.budget : a.capacity - a.budget;
   a.max_moves = most > 0 ? most : 0;
   a.moves = (int32_t*)workspace;
-  // up to 256 KB of K and V to move for a request: by its selecting workgroup, a launch less
-  a.fused = a.max_moves <= FUSED_MOVES && (long long)a.max_moves * a.row_chunks * 32 <= 256 * 1024;
-  const int lds = (a.capacity + 63) / 64 * 16;
-#define LZ_EVICT(THREADS, ITEMS)                                                                                   \
-  do {                                                                                                             \
-    auto kern = evict_select_kernel<THREADS, ITEMS>;                                                               \
-    if (lds > 32768) {                                                                                             \
-      hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);      \
-      if (e != hipSuccess) return e;                                                                               \
-    }                                                                                                              \
-    hipLaunchKernelGGL(kern, dim3(a.batch), dim3(THREADS), lds, st, a);                                            \
-  } while (0)
-  if (a.capacity <= 1024) LZ_EVICT(256, 4);
-  else if (a.capacity <= 4096) LZ_EVICT(512, 8);
-  else if (a.capacity <= 16384) LZ_EVICT(1024, 16);
-  else LZ_EVICT(1024, 0);
-#undef LZ_EVICT
+  if (a.capacity > SELECT_CAPACITY) {
+    a.long_state = (char*)workspace + move_bytes(a.batch, a.capacity, a.budget);
+    const dim3 grid((a.capacity + SEG - 1) / SEG, a.batch);
+    hipLaunchKernelGGL(evict_long_top_kernel, grid, dim3(SEG_THREADS), 0, st, a);
+    hipLaunchKernelGGL(evict_long_pass_kernel<0>, grid, dim3(SEG_THREADS), 0, st, a);
+    hipLaunchKernelGGL(evict_long_pass_kernel<1>, grid, dim3(SEG_THREADS), 0, st, a);
+    hipLaunchKernelGGL(evict_long_pass_kernel<2>, grid, dim3(SEG_THREADS), 0, st, a);
+    hipLaunchKernelGGL(evict_long_pass_kernel<PASSES>, grid, dim3(SEG_THREADS), 0, st, a);
+    hipLaunchKernelGGL(evict_long_moves_kernel, dim3(a.batch), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(evict_long_tables_kernel, dim3(grid.x, a.batch), dim3(256), 0, st, a);
+  } else {
+    // up to 256 KB of K and V to move for a request: by its selecting workgroup, a launch less
+    a.fused = a.max_moves <= FUSED_MOVES && (long long)a.max_moves * a.row_chunks * 32 <= 256 * 1024;
+    if (a.capacity <= 1024) hipLaunchKernelGGL((evict_select_kernel<256, 4>), dim3(a.batch), dim3(256), 0, st, a);
+    else if (a.capacity <= 4096) hipLaunchKernelGGL((evict_select_kernel<512, 8>), dim3(a.batch), dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((evict_select_kernel<1024, 16>), dim3(a.batch), dim3(1024), 0, st, a);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.max_moves == 0 || a.fused) return e;
   int groups = 2048 / a.batch;

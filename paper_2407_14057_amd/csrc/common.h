@@ -373,7 +373,7 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
                                         int prefix_len, bool weights);
 hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan& plan, int head_dim, void* workspace, hipStream_t st);
 
-constexpr int EVICT_MAX_CAPACITY = 1 << 19;          // two bits a slot in the 160 KB of LDS
+constexpr int EVICT_MAX_CAPACITY = 1 << 24;
 struct EvictArgs {
   uint16_t *k, *v;
   long long batch_stride, row_stride;
@@ -385,6 +385,7 @@ struct EvictArgs {
   int32_t *pos_out, *lengths_out, *kept, *status;
   int32_t* moves;                      // workspace: [batch] counts, then per request holes[max_moves], movers[max_moves]
   int max_moves, fused;                // fused: the selecting workgroup moves the rows too
+  void* long_state;                    // workspace of caches that one workgroup does not select from
 };
 size_t evict_workspace_bytes(int batch, int capacity, int budget);
 hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st);

@@ -427,6 +427,14 @@ def test_eviction_of_one_request(n, budget):
         Cache([n], n, seed=n, values=values).run_and_check(budget, min(2, budget // 2), budget // 3)
 
 
+@pytest.mark.parametrize("values", ["tied", "equal", "odd", "spread"])
+def test_eviction_from_caches_that_several_workgroups_select_from(values):
+    lengths = [16385, 0, -1, 7, 8192, 8193, 300, 16500, 16384, 12000]
+    Cache(lengths, 16500, seed=11, values=values).run_and_check(250, 4, 60)
+    Cache(lengths, 16500, seed=12, values=values).run_and_check(8193, 4, 60, in_place=True)
+    Cache(lengths, 16500, seed=13, values=values).run_and_check(16384, 0, 5000)
+
+
 def test_eviction_over_many_words():
     """More 64-slot words than a workgroup has threads."""
     Cache([200000], 200000, heads=(1, 64), seed=6, values="spread").run_and_check(150000, 4, 1000)
@@ -455,8 +463,9 @@ def test_more_protected_tokens_than_the_budget():
     c.run_and_check(10, 0, 10)
 
 
-def test_captured_eviction_replays():
-    c = Cache([300, 200], 300, seed=8, values="spread")
+@pytest.mark.parametrize("capacity", [300, 17000])
+def test_captured_eviction_replays(capacity):
+    c = Cache([300, 200] if capacity == 300 else [16900, 200], capacity, seed=8, values="spread")
     ws = torch.empty(B.lazyllm_op_cache_evict_workspace_bytes(c.cache, 100), dtype=torch.uint8, device=DEV)
     outs = [torch.zeros_like(c.weight), torch.zeros_like(c.pos), torch.zeros_like(c.len_dev)]
     call = lambda stream: B.lazyllm_op_cache_evict(c.cache, c.weight, c.pos, c.len_dev, 100, 2, 10, *outs, ws, stream=stream)  # noqa: E731

@@ -90,7 +90,7 @@ def _evict(cache=None, size=1 << 40, **change):
 def test_eviction_refuses_bad_arguments():
     for change in BAD_CACHES + BAD_ROWS:
         assert _evict(_cache(**change)) == B.LAZYLLM_EINVAL, change
-    assert _evict(_cache(batch=1, capacity=524289)) == B.LAZYLLM_EINVAL
+    assert _evict(_cache(batch=1, capacity=(1 << 24) + 1)) == B.LAZYLLM_EINVAL
     for name in ("weight", "pos", "lengths", "weight_out", "pos_out", "lengths_out", "workspace"):
         assert _evict(**{name: None}) == B.LAZYLLM_EINVAL, name
     for change in (dict(budget=0), dict(budget=-1), dict(sinks=-1), dict(recent=-1), dict(sinks=401), dict(budget=3, sinks=2, recent=2),
@@ -100,7 +100,7 @@ def test_eviction_refuses_bad_arguments():
     assert size > 0 and _evict(size=size - 1) == B.LAZYLLM_ENOSPC and _evict(size=0) == B.LAZYLLM_ENOSPC
     assert B.lazyllm_op_cache_evict_workspace_bytes(_cache(), 0) == 0
     assert B.lazyllm_op_cache_evict_workspace_bytes(_cache(head_dim=96), 10) == 0
-    assert B.lazyllm_op_cache_evict_workspace_bytes(_cache(batch=1, capacity=524289), 10) == 0
+    assert B.lazyllm_op_cache_evict_workspace_bytes(_cache(batch=1, capacity=(1 << 24) + 1), 10) == 0
     assert B.lib().lazyllm_op_cache_evict(None, ONE, ONE, ONE, 5, 0, 0, ONE, ONE, ONE, None, None, ONE, 1 << 30, None) == B.LAZYLLM_EINVAL
 
 
