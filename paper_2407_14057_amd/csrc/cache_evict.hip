@@ -160,6 +160,13 @@ __device__ __forceinline__ int resolve_moves(unsigned long long* keep, const uns
 
 }  // namespace
 
+__device__ __forceinline__ void move_tables(const EvictArgs& a, int b, int to, int from) {
+  const size_t at = (size_t)b * a.capacity;
+  a.weight_out[at + to] = a.weight[at + from];
+  a.pos_out[at + to] = a.pos[at + from];
+  if (a.kept != nullptr) a.kept[(size_t)b * a.budget + to] = from;
+}
+
 // THREADS threads, ITEMS slots per thread in registers.  Every wave reads the histograms for itself: a barrier a pass.
 template <int THREADS, int ITEMS>
 __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
@@ -174,24 +181,26 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
   float* weight_out = a.weight_out + (size_t)b * a.capacity;
   int32_t* pos_out = a.pos_out + (size_t)b * a.capacity;
   int32_t* kept_from = a.kept != nullptr ? a.kept + (size_t)b * a.budget : nullptr;
-  const int given = a.lengths[b], n = min(given, a.capacity), kept = min(n, a.budget);
-  for (int i = threadIdx.x; i < PASSES * BINS / 4; i += THREADS) ((int4*)hist)[i] = make_int4(0, 0, 0, 0);
-
+  // the tables are on their way before the length is known
   float w[ITEMS];
   int p[ITEMS];
   uint32_t keys[ITEMS];
+#pragma unroll
+  for (int u = 0; u < ITEMS; ++u) {
+    const int i = u * THREADS + threadIdx.x;
+    w[u] = i < a.capacity ? weight[i] : 0.f;
+    p[u] = i < a.capacity ? pos[i] : 0;
+  }
+  const int given = a.lengths[b], n = min(given, a.capacity), kept = min(n, a.budget);
+  for (int i = threadIdx.x; i < PASSES * BINS / 4; i += THREADS) ((int4*)hist)[i] = make_int4(0, 0, 0, 0);
   // calls f(item, slot) for the items that any thread has a slot below n for; all lanes of a wave together
   auto each = [&](auto f) {
 #pragma unroll
     for (int u = 0; u < ITEMS; ++u)
       if (u * THREADS < n) f(u, u * THREADS + (int)threadIdx.x);
   };
-  each([&](int u, int i) {
-    w[u] = i < n ? weight[i] : 0.f;
-    p[u] = i < n ? pos[i] : INT32_MIN;
-  });
   int top = INT32_MIN;
-  each([&](int u, int) { top = max(top, p[u]); });
+  each([&](int u, int i) { top = max(top, i < n ? p[u] : INT32_MIN); });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
   if (lane == 0) part[wave].x = top;
@@ -243,14 +252,9 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
   if (threadIdx.x == 0 && !a.fused) a.moves[b] = holes;
   if (new_weight || new_pos || kept_from != nullptr)
     each([&](int u, int i) { if (i < kept && ((keep[i >> 6] >> (i & 63)) & 1ull)) stay(u, i); });
-  __syncthreads();                        // the lists are read by other threads of this workgroup
-  for (int i = threadIdx.x; i < holes; i += THREADS) {
-    const int to = hole_at[i], from = mover_at[i];
-    weight_out[to] = weight[from];
-    pos_out[to] = pos[from];
-    if (kept_from != nullptr) kept_from[to] = from;
-  }
   if (!a.fused) return;
+  __syncthreads();                        // the lists are read by other threads of this workgroup
+  for (int i = threadIdx.x; i < holes; i += THREADS) move_tables(a, b, hole_at[i], mover_at[i]);
   uint16_t* k = a.k + b * a.batch_stride;
   uint16_t* v = a.v + b * a.batch_stride;
   for (int i = threadIdx.x; i < holes * a.row_chunks; i += THREADS) {
@@ -271,12 +275,12 @@ constexpr int SEG = 8192, SEG_THREADS = 512, SEG_ITEMS = SEG / SEG_THREADS;
 namespace {
 
 struct LongState {                       // of one request, in the workspace
-  int32_t *top, *hist, *kept;
+  int32_t *top, *hist, *found;           // found: duplicates of the threshold to keep, all of them, tokens kept
   unsigned long long *keep, *equal;
 };
 __host__ __device__ inline size_t long_state_bytes(int capacity) {
   const size_t segs = (capacity + SEG - 1) / SEG;
-  return PASSES * BINS * 4 + segs * (SEG / 64) * 16 + ((segs + 1) * 4 + 255) / 256 * 256;
+  return PASSES * BINS * 4 + segs * (SEG / 64) * 16 + ((segs + 3) * 4 + 255) / 256 * 256;
 }
 __device__ __forceinline__ LongState long_state(const EvictArgs& a, int b) {
   const size_t segs = (a.capacity + SEG - 1) / SEG;
@@ -286,7 +290,7 @@ __device__ __forceinline__ LongState long_state(const EvictArgs& a, int b) {
   s.keep = (unsigned long long*)(at + PASSES * BINS * 4);
   s.equal = s.keep + segs * (SEG / 64);
   s.top = (int32_t*)(s.equal + segs * (SEG / 64));
-  s.kept = s.top + segs;
+  s.found = s.top + segs;
   return s;
 }
 // Highest position of a request, from its segments'; all threads of a wave together.
@@ -368,6 +372,10 @@ __global__ void __launch_bounds__(SEG_THREADS) evict_long_pass_kernel(EvictArgs 
       }
     }
   }
+  if (PASS == PASSES && seg == 0 && threadIdx.x == 0) {
+    s.found[0] = f.need;
+    s.found[1] = f.same;
+  }
   if (PASS < PASSES) {
     __syncthreads();
     for (int i = threadIdx.x; i < pass_bins(PASS); i += SEG_THREADS)
@@ -384,49 +392,21 @@ __global__ void __launch_bounds__(1024) evict_long_moves_kernel(EvictArgs a) {
   __syncthreads();                       // every thread has read the length, which may be overwritten now
   int holes = 0;
   if (n > a.budget) {
-    Found f;
-    f.need = kept;
-#pragma unroll
-    for (int pass = 0; pass < PASSES; ++pass) next_digit(f, s.hist + pass * BINS, pass);
     int32_t* hole_at = a.moves + a.batch + (size_t)b * 2 * a.max_moves;
-    holes = resolve_moves<1024>(s.keep, s.equal, (n + 63) / 64, kept, f.need, f.need == f.same, hole_at, hole_at + a.max_moves, part);
+    holes = resolve_moves<1024>(s.keep, s.equal, (n + 63) / 64, kept, s.found[0], s.found[0] == s.found[1], hole_at,
+                                hole_at + a.max_moves, part);
   }
   if (threadIdx.x == 0) {
     a.moves[b] = holes;
-    *s.kept = kept;
+    s.found[2] = kept;
     a.lengths_out[b] = kept;
     if (given > a.capacity && a.status != nullptr) atomicOr(a.status, ST_BAD_CU);
   }
 }
 
-// The tables of the kept tokens: of those that stay where they are, unless the table is its own output, and of those that move.
-__global__ void __launch_bounds__(256) evict_long_tables_kernel(EvictArgs a) {
-  const int b = blockIdx.y, threads = gridDim.x * 256, first = blockIdx.x * 256 + threadIdx.x;
-  const LongState s = long_state(a, b);
-  const int kept = *s.kept, holes = a.moves[b];
-  const float* weight = a.weight + (size_t)b * a.capacity;
-  const int32_t* pos = a.pos + (size_t)b * a.capacity;
-  float* weight_out = a.weight_out + (size_t)b * a.capacity;
-  int32_t* pos_out = a.pos_out + (size_t)b * a.capacity;
-  int32_t* kept_from = a.kept != nullptr ? a.kept + (size_t)b * a.budget : nullptr;
-  const bool all_stay = holes == 0;
-  if (weight_out != weight || pos_out != pos || kept_from != nullptr)
-    for (int i = first; i < kept; i += threads)
-      if (all_stay || ((s.keep[i >> 6] >> (i & 63)) & 1ull)) {
-        if (weight_out != weight) weight_out[i] = weight[i];
-        if (pos_out != pos) pos_out[i] = pos[i];
-        if (kept_from != nullptr) kept_from[i] = i;
-      }
-  const int32_t* hole_at = a.moves + a.batch + (size_t)b * 2 * a.max_moves;
-  for (int i = first; i < holes; i += threads) {
-    const int to = hole_at[i], from = hole_at[a.max_moves + i];
-    weight_out[to] = weight[from];
-    pos_out[to] = pos[from];
-    if (kept_from != nullptr) kept_from[to] = from;
-  }
-}
-
-// K and V of the tokens that move, a row at a time.
+// The tokens that move, a row of K and V at a time.  LONG: the tables of those that stay, unless a table is its own output,
+// are written here too.
+template <bool LONG>
 __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
   const int b = blockIdx.y, count = a.moves[b];
   const int32_t* hole_at = a.moves + a.batch + (size_t)b * 2 * a.max_moves;
@@ -434,13 +414,24 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
   uint16_t* k = a.k + b * a.batch_stride;
   uint16_t* v = a.v + b * a.batch_stride;
   for (int i = blockIdx.x; i < count; i += gridDim.x) {
-    const long long to = hole_at[i] * a.row_stride, from = mover_at[i] * a.row_stride;
+    const int to = hole_at[i], from = mover_at[i];
+    const long long k_to = to * a.row_stride, k_from = from * a.row_stride;
     for (int ch = threadIdx.x; ch < a.row_chunks; ch += 256) {
-      const uint4 x = *(const uint4*)(k + from + 8 * ch), y = *(const uint4*)(v + from + 8 * ch);
-      *(uint4*)(k + to + 8 * ch) = x;
-      *(uint4*)(v + to + 8 * ch) = y;
+      const uint4 x = *(const uint4*)(k + k_from + 8 * ch), y = *(const uint4*)(v + k_from + 8 * ch);
+      *(uint4*)(k + k_to + 8 * ch) = x;
+      *(uint4*)(v + k_to + 8 * ch) = y;
     }
+    if (threadIdx.x == 0) move_tables(a, b, to, from);
   }
+  if (!LONG || (a.weight_out == a.weight && a.pos_out == a.pos && a.kept == nullptr)) return;
+  const LongState s = long_state(a, b);
+  const size_t at = (size_t)b * a.capacity;
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < s.found[2]; i += gridDim.x * 256)
+    if (count == 0 || ((s.keep[i >> 6] >> (i & 63)) & 1ull)) {          // (without moves all of them stay)
+      if (a.weight_out != a.weight) a.weight_out[at + i] = a.weight[at + i];
+      if (a.pos_out != a.pos) a.pos_out[at + i] = a.pos[at + i];
+      if (a.kept != nullptr) a.kept[(size_t)b * a.budget + i] = i;
+    }
 }
 
 // The largest capacity that one workgroup selects from: up to here its launch is the quicker one (16000 slots: 28 us, of
@@ -469,7 +460,6 @@ hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st) {
     hipLaunchKernelGGL(evict_long_pass_kernel<2>, grid, dim3(SEG_THREADS), 0, st, a);
     hipLaunchKernelGGL(evict_long_pass_kernel<PASSES>, grid, dim3(SEG_THREADS), 0, st, a);
     hipLaunchKernelGGL(evict_long_moves_kernel, dim3(a.batch), dim3(1024), 0, st, a);
-    hipLaunchKernelGGL(evict_long_tables_kernel, dim3(grid.x, a.batch), dim3(256), 0, st, a);
   } else {
     // up to 256 KB of K and V to move for a request: by its selecting workgroup, a launch less
     a.fused = a.max_moves <= FUSED_MOVES && (long long)a.max_moves * a.row_chunks * 32 <= 256 * 1024;
@@ -477,12 +467,15 @@ hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st) {
     else if (a.capacity <= 4096) hipLaunchKernelGGL((evict_select_kernel<512, 8>), dim3(a.batch), dim3(512), 0, st, a);
     else hipLaunchKernelGGL((evict_select_kernel<1024, 16>), dim3(a.batch), dim3(1024), 0, st, a);
   }
+  const bool one_workgroup = a.capacity <= SELECT_CAPACITY;
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.max_moves == 0 || a.fused) return e;
+  if (e != hipSuccess || (one_workgroup && (a.max_moves == 0 || a.fused))) return e;
   int groups = 2048 / a.batch;
   if (groups < 16) groups = 16;
-  if (groups > a.max_moves) groups = a.max_moves;
-  hipLaunchKernelGGL(evict_move_kernel, dim3(groups, a.batch), dim3(256), 0, st, a);
+  const int useful = one_workgroup ? a.max_moves : a.max_moves + (a.capacity + 255) / 256;
+  if (groups > useful) groups = useful;
+  if (one_workgroup) hipLaunchKernelGGL(evict_move_kernel<false>, dim3(groups, a.batch), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(evict_move_kernel<true>, dim3(groups, a.batch), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
