@@ -19,7 +19,7 @@ namespace {
 constexpr int STEP = 32;              // keys of a wave's step
 constexpr int WAVES = 4;
 
-// (row of q, query head) of row r of an item: tok = tok0 + r / group, head = kvh * group + r % group
+// Row r of an item is token tok0 + r / group, query head kvh * group + r % group.
 struct Item {
   const uint16_t *k, *v;              // first key of the segment, this K,V head
   const uint16_t *k_tail, *v_tail;    // keys n and up: the new tokens (the prefix: its last row again, masked)
@@ -77,77 +77,83 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
   // The K,V head varies fastest: workgroups are dealt out to the XCDs in turn, so that ranges that a short request does
   // not have leave all XCDs with less to do (parts fastest: 8 requests of 1 - 8 k tokens 165 us, now 127), and row
   // blocks of one range share an L2.
+  int id = blockIdx.x;
+  const int prefix_items = a.shared_tiles ? 0 : a.prefix_parts * a.n_kv * a.prefix_blocks;
   Item it;
-  int b = 0;
-  {
-    int id = blockIdx.x;
-    const int prefix_items = a.shared_tiles ? 0 : a.prefix_parts * a.n_kv * a.prefix_blocks;
-    it.own = id >= prefix_items;
-    if (!it.own) {
-      it.kvh = id % a.n_kv;
-      id /= a.n_kv;
-      it.row0 = id % a.prefix_blocks * 16 * T;
-      it.part = id / a.prefix_blocks;
-      it.n_rows = a.batch * a.q_len * a.group;
-      it.tok0 = 0;
-      it.stride = a.prefix_stride;
-      it.k = a.prefix_k + it.kvh * HD;
-      it.v = a.prefix_v + it.kvh * HD;
-      it.n = a.prefix_len;
-      it.n_tail = 1;
-      it.k_tail = it.k + (a.prefix_len - 1) * it.stride;
-      it.v_tail = it.v + (a.prefix_len - 1) * it.stride;
-      it.tail_stride = 0;
-      it.lo = it.part * a.prefix_range;
-      it.hi = min(it.lo + a.prefix_range, a.prefix_len);
-    } else {
-      id -= prefix_items;
-      it.kvh = id % a.n_kv;
-      id /= a.n_kv;
-      it.row0 = id % a.own_blocks * 16 * T;
-      id /= a.own_blocks;
-      b = id % a.batch;
-      const int part = id / a.batch;
-      it.part = a.prefix_parts + part;
-      it.n_rows = a.q_len * a.group;
-      it.tok0 = b * a.q_len;
-      it.n = cached_tokens(a, b);
-      if (it.n < 0) {
-        // no partial results: the output rows are zero (with more than one part the second launch clears them)
-        if (a.merge == 0)
-          for (int i = threadIdx.x; i < min(16 * T, it.n_rows - it.row0) * (HD / 8); i += 256) {
-            const int r = it.row0 + i / (HD / 8);
-            ((uint4*)(a.o + ((size_t)(it.tok0 + r / a.group) * a.n_heads + it.kvh * a.group + r % a.group) * HD))[i % (HD / 8)] =
-                make_uint4(0, 0, 0, 0);
-          }
-        return;
-      }
-      if (part == 0 && it.kvh == 0 && it.row0 == 0 && threadIdx.x == 0 && a.status != nullptr && a.lengths[b] > a.max_len)
-        atomicOr(a.status, ST_BAD_CU);
-      it.stride = a.row_stride;
-      it.k = a.k + b * a.batch_stride + it.kvh * HD;
-      it.v = a.v + b * a.batch_stride + it.kvh * HD;
-      it.n_tail = a.q_len;
-      it.k_tail = a.k_new + ((size_t)it.tok0 * a.n_kv + it.kvh) * HD;
-      it.v_tail = a.v_new + ((size_t)it.tok0 * a.n_kv + it.kvh) * HD;
-      it.tail_stride = kvd;
-      it.lo = part * a.own_range;
-      it.hi = min(it.lo + a.own_range, it.n + a.q_len);
-    }
+  it.own = id >= prefix_items;
+  if (it.own) id -= prefix_items;
+  it.kvh = id % a.n_kv;
+  id /= a.n_kv;
+  const int blocks = it.own ? a.own_blocks : a.prefix_blocks;
+  it.row0 = 0;
+  if (blocks > 1) {
+    it.row0 = id % blocks * 16 * T;
+    id /= blocks;
   }
-  if (it.lo >= it.hi) return;
+  int b = 0;
+  if (it.own && a.batch > 1) {
+    b = id % a.batch;
+    id /= a.batch;
+  }
+  const int part = id;
+  it.tok0 = b * a.q_len;
+  it.n_rows = (it.own ? 1 : a.batch) * a.q_len * a.group;
 
+  // (on its way while the length is)
   bf16x8_t qf[T][KS];
-  int last[T];                          // the last key that a query row sees
+  int tok[T];
   size_t out_row[T];
 #pragma unroll
   for (int t = 0; t < T; ++t) {
-    const int r = min(it.row0 + 16 * t + c, it.n_rows - 1), tok = r / a.group;
-    out_row[t] = (size_t)(it.tok0 + tok) * a.n_heads + it.kvh * a.group + r % a.group;
+    const int r = min(it.row0 + 16 * t + c, it.n_rows - 1);
+    tok[t] = r / a.group;
+    out_row[t] = (size_t)(it.tok0 + tok[t]) * a.n_heads + it.kvh * a.group + r - tok[t] * a.group;
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[t][s] = *(const bf16x8_t*)(a.q + out_row[t] * HD + 32 * s + 8 * g);
-    last[t] = it.own ? it.n + tok : it.n - 1;
   }
+
+  if (!it.own) {
+    it.part = part;
+    it.stride = a.prefix_stride;
+    it.k = a.prefix_k + it.kvh * HD;
+    it.v = a.prefix_v + it.kvh * HD;
+    it.n = a.prefix_len;
+    it.n_tail = 1;
+    it.k_tail = it.k + (a.prefix_len - 1) * it.stride;
+    it.v_tail = it.v + (a.prefix_len - 1) * it.stride;
+    it.tail_stride = 0;
+    it.lo = part * a.prefix_range;
+    it.hi = min(it.lo + a.prefix_range, a.prefix_len);
+  } else {
+    it.part = a.prefix_parts + part;
+    const int given = a.lengths[b];
+    it.n = min(given, a.max_len);
+    if (it.n < 0) {
+      // no partial results: the output rows are zero (with more than one part the second launch clears them)
+      if (a.merge == 0)
+        for (int i = threadIdx.x; i < min(16 * T, it.n_rows - it.row0) * (HD / 8); i += 256) {
+          const int r = it.row0 + i / (HD / 8);
+          ((uint4*)(a.o + ((size_t)(it.tok0 + r / a.group) * a.n_heads + it.kvh * a.group + r % a.group) * HD))[i % (HD / 8)] =
+              make_uint4(0, 0, 0, 0);
+        }
+      return;
+    }
+    if (part == 0 && it.kvh == 0 && it.row0 == 0 && threadIdx.x == 0 && a.status != nullptr && given > a.max_len)
+      atomicOr(a.status, ST_BAD_CU);
+    it.stride = a.row_stride;
+    it.k = a.k + b * a.batch_stride + it.kvh * HD;
+    it.v = a.v + b * a.batch_stride + it.kvh * HD;
+    it.n_tail = a.q_len;
+    it.k_tail = a.k_new + ((size_t)it.tok0 * a.n_kv + it.kvh) * HD;
+    it.v_tail = a.v_new + ((size_t)it.tok0 * a.n_kv + it.kvh) * HD;
+    it.tail_stride = kvd;
+    it.lo = part * a.own_range;
+    it.hi = min(it.lo + a.own_range, it.n + a.q_len);
+  }
+  if (it.lo >= it.hi) return;
+  int last[T];                          // the last key that a query row sees
+#pragma unroll
+  for (int t = 0; t < T; ++t) last[t] = it.own ? it.n + tok[t] : it.n - 1;
 
   floatx4_t acc[T][NT];
   float m_run[T], l_run[T];
@@ -356,27 +362,36 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) 
     const int row = a.merge == 1 ? blockIdx.x * WAVES + wave : blockIdx.x;
     const int first = a.merge == 1 ? 0 : wave, step = a.merge == 1 ? 1 : WAVES;
     if (row >= all_rows) return;       // (of whole waves, and only where no barrier follows)
-    const int n = cached_tokens(a, row / (a.q_len * a.n_heads));
-    const int parts = n < 0 ? 0 : a.prefix_parts + (n + a.q_len + a.own_range - 1) / a.own_range;
     const float2* st = a.stat + row;
-    const float2 ml = merged_stat(st, all_rows, parts, lane & 7);
-    float x[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = 0.f;
     const float* src = a.part + (size_t)row * HD + E * lane;
-    for (int s0 = first; s0 < parts; s0 += 4 * step) {
-      float w[4], v[4][E];
+    const int most = a.prefix_parts + a.own_parts;
+    // the parts' outputs four at a time, the next four on their way before the sum of these (and the first before anything
+    // is known about the request: those it does not have are not added)
+    float x[E], v[4][E], top[4];
+    auto fetch = [&](int s0) {
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int s = min(s0 + u * step, parts - 1);
-        w[u] = s0 + u * step < parts ? __builtin_amdgcn_exp2f(st[(size_t)s * all_rows].x - ml.x) : 0.f;
+        const size_t s = min(s0 + u * step, most - 1);
+        top[u] = st[s * all_rows].x;
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[u][e] = src[(size_t)s * all_rows * HD + e];
+        for (int e = 0; e < E; ++e) v[u][e] = src[s * all_rows * HD + e];
       }
+    };
+    fetch(first);
+    const int n = cached_tokens(a, row / (a.q_len * a.n_heads));
+    const int parts = n < 0 ? 0 : a.prefix_parts + (n + a.q_len + a.own_range - 1) / a.own_range;
+    const float2 ml = merged_stat(st, all_rows, parts, lane & 7);
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = 0.f;
+    for (int s0 = first; s0 < parts; s0 += 4 * step) {
 #pragma unroll
       for (int u = 0; u < 4; ++u)
+        if (s0 + u * step < parts) {
+          const float w = __builtin_amdgcn_exp2f(top[u] - ml.x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] += w[u] * v[u][e];
+          for (int e = 0; e < E; ++e) x[e] += w * v[u][e];
+        }
+      if (s0 + 4 * step < parts) fetch(s0 + 4 * step);
     }
     if (a.merge != 1) {
 #pragma unroll
