@@ -534,7 +534,7 @@ int lazyllm_op_gather(const void* h, const int32_t* pos, const int32_t* keep_idx
  * [n_kv_heads, head_dim].  The order of a request's slots means nothing to the attention.  head_dim 64 or
  * 128; strides multiples of 8; row_stride from n_kv_heads * head_dim to 2^24; batch_stride at least
  * row_stride * (capacity - 1) + n_kv_heads * head_dim, so that no two rows overlap (unused with batch 1);
- * batch * capacity below 2^31.  Rows beyond a request's length are not read. */
+ * capacity up to 2^30, batch * capacity below 2^31.  Rows beyond a request's length are not read. */
 typedef struct lazyllm_kv_cache {
   void* k;
   void* v;
@@ -558,12 +558,14 @@ typedef struct lazyllm_kv_cache {
  *             slot without the first term.  Slots beyond the new length are not written.  May be the same table.
  *   pos_new,  both or neither: pos_new int32 [batch] is the original position of a request's first new token; the
  *   pos       new tokens' positions are written into pos int32 [batch, capacity].
- *   prefix_*  lazyllm_op_prefix_attention only: K and V rows of prefix_len tokens that every request has in front of
- *             its cache, prefix_stride elements from row to row (as row_stride), e.g. result.k[l], result.v[l] of a
- *             prefill of the common prompt.
+ *   prefix_*  lazyllm_op_prefix_attention only: K and V rows of prefix_len (up to 2^30) tokens that every request has
+ *             in front of its cache, prefix_stride elements from row to row (as row_stride), e.g. result.k[l] and
+ *             result.v[l] of a prefill of the common prompt.
  * New token t of a request sees the prefix, the request's cached tokens and its new tokens up to t.  Keys and
  * values that some new token of a request sees must be finite; what lies elsewhere is of no account.
- * Sums and softmax statistics are fp32; o is rounded once.  The same call gives the same bits every time. */
+ * Sums and softmax statistics are fp32 and o is rounded once; a probability enters the product with V as two bf16
+ * terms (value and remainder), against a prefix of many query rows as one.  The same call gives the same bits every
+ * time; other lengths' bounds, another batch or a prefix can change the order of a row's sums. */
 typedef struct lazyllm_step_attention {
   const void *q, *k_new, *v_new;
   void* o;
@@ -580,7 +582,8 @@ typedef struct lazyllm_step_attention {
 } lazyllm_step_attention;
 
 /* Bytes of workspace (device, 256-byte aligned) of a step: prefix_len 0 for lazyllm_op_cache_attention; weights:
- * whether weight_out is given.  Host only.  0 on a bad argument.  Nothing in it needs to be cleared. */
+ * whether weight_out is given (4 bytes for every query row, head and slot then).  Host only.  0 on a bad argument.  Nothing
+ * in it needs to be cleared, and nothing in it outlives the call. */
 size_t lazyllm_op_cache_attention_workspace_bytes(const lazyllm_kv_cache* cache, int32_t n_heads, int32_t q_len,
                                                   int32_t max_len, int32_t prefix_len, int32_t weights);
 

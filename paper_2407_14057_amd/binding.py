@@ -483,7 +483,8 @@ def lazyllm_op_cache_attention(cache, q, k_new, v_new, lengths, n_heads, q_len, 
 def lazyllm_op_prefix_attention(cache, prefix_k, prefix_v, q, k_new, v_new, lengths, n_heads, q_len, max_len, o, workspace,
                                 weight=None, weight_out=None, pos_new=None, pos=None, status=None, stream=None) -> None:
     """prefix_k, prefix_v: [prefix_len, n_kv_heads, head_dim], possibly strided from row to row."""
-    if prefix_k.shape != prefix_v.shape or prefix_k.stride() != prefix_v.stride() or not prefix_k[0].is_contiguous():
+    if (prefix_k.shape != prefix_v.shape or prefix_k.stride() != prefix_v.stride() or prefix_k.dim() != 3 or
+            prefix_k.shape[0] < 1 or prefix_k.shape[1:] != (cache.n_kv_heads, cache.head_dim) or not prefix_k[0].is_contiguous()):
         raise LazyLLMError(LAZYLLM_EINVAL)
     row = prefix_k.stride(0) if prefix_k.shape[0] > 1 else prefix_k[0].numel()
     s = lazyllm_step_attention(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(o), _ptr(lengths), n_heads, q_len, max_len,

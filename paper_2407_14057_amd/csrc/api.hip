@@ -104,7 +104,7 @@ bool row_stride_ok(int64_t stride, int n_kv_heads, int head_dim) {
 }
 bool kv_cache_shape_ok(const lazyllm_kv_cache* c) {
   return c != nullptr && (c->head_dim == 64 || c->head_dim == 128) && c->n_kv_heads >= 1 && c->n_kv_heads <= 256 &&
-         c->batch >= 1 && c->batch <= 65535 && c->capacity >= 1 && (int64_t)c->batch * c->capacity <= 0x7fffffff;
+         c->batch >= 1 && c->batch <= 65535 && c->capacity >= 1 && c->capacity <= (1 << 30) && (int64_t)c->batch * c->capacity <= 0x7fffffff;
 }
 bool kv_cache_ok(const lazyllm_kv_cache* c) {
   if (!kv_cache_shape_ok(c) || !rows_ok(c->k) || !rows_ok(c->v)) return false;
@@ -123,6 +123,7 @@ int step_attention(const lazyllm_kv_cache* c, const lazyllm_step_attention& s, v
   if ((s.weight == nullptr) != (s.weight_out == nullptr) || (s.pos == nullptr) != (s.pos_new == nullptr)) return LAZYLLM_EINVAL;
   const CacheAttentionPlan plan = cache_attention_plan(c->batch, s.n_heads, c->n_kv_heads, c->head_dim, s.q_len, s.max_len,
                                                        s.prefix_len, s.weight != nullptr);
+  if (!plan.fits) return LAZYLLM_EINVAL;
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0) return LAZYLLM_EINVAL;
   if (ws_bytes < plan.bytes()) return LAZYLLM_ENOSPC;
   CacheAttentionArgs a{};
@@ -1391,9 +1392,9 @@ int lazyllm_op_gather(const void* h, const int32_t* pos, const int32_t* keep_idx
 
 size_t lazyllm_op_cache_attention_workspace_bytes(const lazyllm_kv_cache* c, int32_t n_heads, int32_t q_len,
                                                   int32_t max_len, int32_t prefix_len, int32_t weights) {
-  if (!kv_cache_shape_ok(c) || !step_shape_ok(c, n_heads, q_len, max_len) || prefix_len < 0) return 0;
-  return align_up(cache_attention_plan(c->batch, n_heads, c->n_kv_heads, c->head_dim, q_len, max_len, prefix_len,
-                                       weights != 0).bytes() + 1);
+  if (!kv_cache_shape_ok(c) || !step_shape_ok(c, n_heads, q_len, max_len) || prefix_len < 0 || prefix_len > (1 << 30)) return 0;
+  const CacheAttentionPlan plan = cache_attention_plan(c->batch, n_heads, c->n_kv_heads, c->head_dim, q_len, max_len, prefix_len, weights != 0);
+  return plan.fits ? align_up(plan.bytes() + 1) : 0;
 }
 
 int lazyllm_op_cache_attention(const lazyllm_kv_cache* cache, const lazyllm_step_attention* step, void* workspace,
@@ -1407,7 +1408,7 @@ int lazyllm_op_cache_attention(const lazyllm_kv_cache* cache, const lazyllm_step
 
 int lazyllm_op_prefix_attention(const lazyllm_kv_cache* cache, const lazyllm_step_attention* step, void* workspace,
                                 size_t ws_bytes, void* hip_stream) {
-  if (step == nullptr || step->prefix_len < 1 || !rows_ok(step->prefix_k) || !rows_ok(step->prefix_v) || cache == nullptr ||
+  if (step == nullptr || step->prefix_len < 1 || step->prefix_len > (1 << 30) || !rows_ok(step->prefix_k) || !rows_ok(step->prefix_v) || cache == nullptr ||
       !row_stride_ok(step->prefix_stride, cache->n_kv_heads, cache->head_dim))
     return LAZYLLM_EINVAL;
   return step_attention(cache, *step, workspace, ws_bytes, (hipStream_t)hip_stream);

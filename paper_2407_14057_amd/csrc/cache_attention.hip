@@ -706,6 +706,15 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
   p.part_bytes = p.merge ? up(all_rows * parts * head_dim * 4) : 0;
   p.stat_bytes = p.merge || weights ? up(all_rows * parts * 8) : 0;
   p.z_bytes = weights ? up(all_rows * p.z_ld * 4) : 0;
+  const size_t prefix_items = (size_t)p.prefix_parts * n_kv * p.prefix_blocks;
+  const size_t items = (size_t)batch * n_kv * p.own_blocks * p.own_parts + (p.shared_tiles ? 0 : prefix_items);
+  const size_t merge_items = (p.merge == 0 ? 0 : p.merge == 1 ? (all_rows + WAVES - 1) / WAVES : all_rows) +
+                             (weights ? (size_t)batch * ((max_len + q_len + 63) / 64) : 0);
+  const size_t most = 0xffffffffull / 512;           // threads of a launch are counted in 32 bits
+  p.fits = prefix_items <= most && items <= most && merge_items <= most && all_rows <= 0x7fffffff;
+  p.prefix_groups = p.shared_tiles ? (unsigned)prefix_items : 0;
+  p.groups = (unsigned)items;
+  p.merge_groups = (unsigned)merge_items;
   return p;
 }
 
@@ -721,13 +730,6 @@ hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan
   a.part = p.part_bytes ? (float*)ws : nullptr;
   a.stat = p.stat_bytes ? (float2*)(ws + p.part_bytes) : nullptr;
   a.z = p.z_bytes ? (float*)(ws + p.part_bytes + p.stat_bytes) : nullptr;
-  const long long prefix_items = (long long)p.prefix_parts * a.n_kv * p.prefix_blocks;
-  const long long items = (long long)a.batch * a.n_kv * p.own_blocks * p.own_parts + (p.shared_tiles ? 0 : prefix_items);
-  const long long all_rows = (long long)a.batch * a.q_len * a.n_heads;
-  const long long merge_groups = (a.merge == 0 ? 0 : a.merge == 1 ? (all_rows + WAVES - 1) / WAVES : all_rows) +
-                                 (a.z != nullptr ? (long long)a.batch * ((a.max_len + a.q_len + 63) / 64) : 0);
-  if (prefix_items > 0x7fffffff || items > 0x7fffffff || all_rows > 0x7fffffff || merge_groups > 0x7fffffff)
-    return hipErrorInvalidValue;
   if (p.shared_tiles) {
 #define LZ_PATT(HD)                                                                                                \
   do {                                                                                                             \
@@ -735,7 +737,7 @@ hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan
     auto kern = prefix_attention_kernel<HD>;                                                                       \
     hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);  \
     if (e != hipSuccess) return e;                                                                                 \
-    hipLaunchKernelGGL(kern, dim3((unsigned)prefix_items), dim3(512), LDS_BYTES, st, a);                           \
+    hipLaunchKernelGGL(kern, dim3(p.prefix_groups), dim3(512), LDS_BYTES, st, a);                           \
     e = hipGetLastError();                                                                                         \
     if (e != hipSuccess) return e;                                                                                 \
   } while (0)
@@ -752,7 +754,7 @@ hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan
       hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES); \
       if (e != hipSuccess) return e;                                                                               \
     }                                                                                                              \
-    hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(64 * WAVES), LDS_BYTES, st, a);                           \
+    hipLaunchKernelGGL(kern, dim3(p.groups), dim3(64 * WAVES), LDS_BYTES, st, a);                           \
   } while (0)
   if (head_dim == 128) {
     if (p.tiles == 1) LZ_CATT(128, 1, true);
@@ -765,9 +767,9 @@ hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan
   }
 #undef LZ_CATT
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || merge_groups == 0) return e;
-  if (head_dim == 128) hipLaunchKernelGGL(cache_merge_kernel<128>, dim3((unsigned)merge_groups), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(cache_merge_kernel<64>, dim3((unsigned)merge_groups), dim3(256), 0, st, a);
+  if (e != hipSuccess || p.merge_groups == 0) return e;
+  if (head_dim == 128) hipLaunchKernelGGL(cache_merge_kernel<128>, dim3(p.merge_groups), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(cache_merge_kernel<64>, dim3(p.merge_groups), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

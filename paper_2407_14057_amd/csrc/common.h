@@ -366,6 +366,8 @@ struct CacheAttentionPlan {
   int own_blocks, own_range, own_parts, prefix_blocks, prefix_range, prefix_parts;
   int merge;                           // 0: one part, no merge; else output rows merged by a wave (1) or a workgroup (2) each
   int z_ld;
+  unsigned prefix_groups, groups, merge_groups;   // workgroups of the three launches; 0: no such launch
+  bool fits;                           // ... are what a launch can have
   size_t part_bytes, stat_bytes, z_bytes;
   size_t bytes() const { return part_bytes + stat_bytes + z_bytes; }
 };

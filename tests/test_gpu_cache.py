@@ -167,6 +167,44 @@ def test_all_requests_idle():
             s.run_and_check()
 
 
+@pytest.mark.parametrize("heads", [(256, 1, 64), (256, 256, 64), (40, 40, 128), (5, 5, 64), (7, 1, 128), (48, 3, 128)])
+def test_attention_of_other_head_counts(heads):
+    Step(heads, [0, 40, -1, 200], 1, seed=21).run_and_check()
+    Step(heads, [0, 40, -1, 200], 3, prefix=77, seed=22).run_and_check()
+
+
+def test_caches_that_are_a_part_of_larger_ones():
+    """Some requests' and some slots' rows of larger buffers: what surrounds them is neither read nor written."""
+    s = Step((4, 2, 64), [0, 100, -1, 33], 3, seed=23)
+    wide = [torch.full((9, s.capacity + 11, 5, 64), NAN, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    views = [w[1:9:2, 4:4 + s.capacity, 1:3] for w in wide]
+    for mine, view, w in ((s.k, views[0], wide[0]), (s.v, views[1], wide[1])):
+        view.copy_(mine)
+    s.k, s.v = views
+    s.cache = B.make_kv_cache(s.k, s.v)
+    s.run_and_check()
+    for w in wide:
+        w[1:9:2, 4:4 + s.capacity, 1:3] = NAN
+        assert bool(w.isnan().all())
+
+
+@pytest.mark.parametrize("prefix", [0, 600])
+def test_two_steps_at_once_on_two_streams(prefix):
+    lengths = [900, 33, -1, 500, 0, 77]
+    alone = [Step((32, 8, 128), lengths, 2, prefix=prefix, seed=24 + i) for i in range(2)]
+    for s in alone:
+        s.run_and_check()
+    both = [Step((32, 8, 128), lengths, 2, prefix=prefix, seed=24 + i) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, stream in zip(both, streams):
+            s.run(stream=stream)
+    torch.cuda.synchronize()
+    for s, a in zip(both, alone):
+        assert torch.equal(s.o, a.o) and torch.equal(s.weight_out, a.weight_out)
+
+
 @pytest.mark.parametrize("heads", list(HEADS))
 @pytest.mark.parametrize("prefix", [1, 31, 32, 33, 129, 700])
 def test_shared_prefix(heads, prefix):
@@ -292,11 +330,13 @@ def test_same_bits_every_time_and_on_another_stream():
             assert torch.equal(a.o, b.o) and torch.equal(a.weight_out, b.weight_out)
 
 
-@pytest.mark.parametrize("prefix", [0, 300])
-def test_captured_step_replays_as_the_lengths_grow(prefix):
+@pytest.mark.parametrize("heads,lengths,prefix", [((4, 2, 64), [100, 0, 257, -1], 0), ((4, 2, 64), [100, 0, 257, -1], 300), ((8, 1, 128), [20, 5, 33, -1], 400),
+                                                  ((32, 1, 128), [3] * 140, 5000)])
+def test_captured_step_replays_as_the_lengths_grow(heads, lengths, prefix):
     """Lengths, positions and inputs live on the device: one captured step serves every later one.  Two graphs share a workspace."""
-    s = Step((4, 2, 64), [100, 0, 257, -1], 1, prefix=prefix, seed=19, max_len=300)
-    eager = Step((4, 2, 64), [100, 0, 257, -1], 1, prefix=prefix, seed=19, max_len=300)
+    s = Step(heads, lengths, 1, prefix=prefix, seed=19, max_len=300)
+    eager = Step(heads, lengths, 1, prefix=prefix, seed=19, max_len=300)
+    assert s.shared_tiles() == (prefix == 5000)
     s.run()                                                     # (loads the kernels outside the capture)
     torch.cuda.synchronize()
     s.weight_out.fill_(-5.0)
@@ -419,6 +459,41 @@ def test_eviction_keeps_the_best(values, budget, sinks, recent):
 def test_eviction_in_place(values):
     c = Cache([300, 12, 0, -3, 301], 301, seed=2, values=values)
     c.run_and_check(70, 3, 9, in_place=True)
+
+
+@pytest.mark.parametrize("capacity", [300, 16400])
+@pytest.mark.parametrize("weight_in_place,pos_in_place", [(True, False), (False, True)])
+def test_eviction_with_one_table_in_place(capacity, weight_in_place, pos_in_place):
+    c = Cache([300, 12, 299], capacity, seed=14)
+    w, p = c.weight.clone(), c.pos.clone()
+    wo = c.weight if weight_in_place else torch.zeros_like(w)
+    po = c.pos if pos_in_place else torch.zeros_like(p)
+    ws = torch.empty(B.lazyllm_op_cache_evict_workspace_bytes(c.cache, 70), dtype=torch.uint8, device=DEV)
+    B.lazyllm_op_cache_evict(c.cache, c.weight, c.pos, c.len_dev, 70, 2, 9, wo, po, c.len_dev, ws)
+    torch.cuda.synchronize()
+    assert c.len_dev.tolist() == [70, 12, 70]
+    for b, n in enumerate(c.lengths):
+        at = torch.tensor(_evict_expected(w[b].cpu().numpy(), p[b].cpu().numpy(), n, 70, 2, 9), device=DEV)
+        assert torch.equal(wo[b, :len(at)], w[b, at]) and torch.equal(po[b, :len(at)], p[b, at])
+
+
+def test_two_evictions_at_once_on_two_streams():
+    pairs = [Cache([3000, 2500, 2000], 3000, seed=15 + i, values="spread") for i in range(2)]
+    streams, outs = [torch.cuda.Stream() for _ in pairs], []
+    torch.cuda.synchronize()
+    for c, stream in zip(pairs, streams):
+        ws = torch.empty(B.lazyllm_op_cache_evict_workspace_bytes(c.cache, 900), dtype=torch.uint8, device=DEV)
+        out = [torch.zeros_like(c.weight), torch.zeros_like(c.pos), torch.zeros_like(c.len_dev)]
+        before = c.k.clone()
+        torch.cuda.synchronize()
+        outs.append((out, before, ws))
+    for c, stream, (out, _, ws) in zip(pairs, streams, outs):
+        B.lazyllm_op_cache_evict(c.cache, c.weight, c.pos, c.len_dev, 900, 4, 100, *out, ws, stream=stream)
+    torch.cuda.synchronize()
+    for c, (out, before, _) in zip(pairs, outs):
+        for b, n in enumerate(c.lengths):
+            at = torch.tensor(_evict_expected(c.weight[b].cpu().numpy(), c.pos[b].cpu().numpy(), n, 900, 4, 100), device=DEV)
+            assert torch.equal(out[1][b, :900], c.pos[b, at]) and torch.equal(c.k[b, :900], before[b, at])
 
 
 @pytest.mark.parametrize("n,budget", [(1, 1), (2, 1), (1024, 1023), (1025, 1024), (2049, 2048), (5000, 4999), (9000, 1000), (70001, 69000), (70000, 33)])

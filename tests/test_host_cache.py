@@ -23,7 +23,7 @@ def _step(**change):
 
 
 BAD_CACHES = [dict(head_dim=96), dict(head_dim=32), dict(n_kv_heads=0), dict(n_kv_heads=257), dict(batch=0), dict(batch=-1), dict(capacity=0),
-              dict(batch=65536), dict(batch=60000, capacity=60000)]
+              dict(batch=65536), dict(batch=60000, capacity=60000), dict(batch=1, capacity=(1 << 30) + 1)]
 BAD_ROWS = [dict(k=0), dict(v=0), dict(k=ONE + 8), dict(v=ONE + 2), dict(row_stride=120), dict(row_stride=132), dict(row_stride=(1 << 24) + 8),
             dict(row_stride=0), dict(row_stride=-128), dict(batch_stride=1000 * 128 - 8), dict(batch_stride=1000 * 128 + 4), dict(batch_stride=0),
             dict(batch_stride=-1000 * 128), dict(batch_stride=1 << 50)]
@@ -32,7 +32,7 @@ BAD_STEPS = [dict(n_heads=0), dict(n_heads=3), dict(n_heads=258), dict(q_len=0),
 BAD_POINTERS = [dict(q=0), dict(k_new=0), dict(v_new=0), dict(o=0), dict(lengths=0), dict(q=ONE + 8), dict(k_new=ONE + 4), dict(v_new=ONE + 2),
                 dict(o=ONE + 8), dict(weight=ONE), dict(weight_out=ONE), dict(pos=ONE), dict(pos_new=ONE)]
 BAD_PREFIXES = [dict(prefix_len=0), dict(prefix_len=-1), dict(prefix_k=0), dict(prefix_v=0), dict(prefix_k=ONE + 8), dict(prefix_v=ONE + 8),
-                dict(prefix_stride=120), dict(prefix_stride=132), dict(prefix_stride=0), dict(prefix_stride=(1 << 24) + 8)]
+                dict(prefix_len=(1 << 30) + 1), dict(prefix_stride=120), dict(prefix_stride=132), dict(prefix_stride=0), dict(prefix_stride=(1 << 24) + 8)]
 
 
 def _attend(name, cache, step, ws=ONE, size=1 << 40):
@@ -74,6 +74,11 @@ def test_workspace_of_the_attention():
     assert B.lib().lazyllm_op_cache_attention_workspace_bytes(None, 4, 2, 100, 0, 0) == 0
     assert size(_cache(), 4, 2, 900, 0, True) > size(_cache(), 4, 2, 900) > 0
     assert size(_cache(), 4, 2, 900, 5000) > size(_cache(), 4, 2, 900)
+    assert size(_cache(), 4, 2, 100, (1 << 30) + 1) == 0
+    # more workgroups than a launch can have
+    assert size(_cache(batch=65535, capacity=20000, batch_stride=20000 * 128), 256, 64, 100) == 0
+    many = _cache(batch=65535, capacity=20000, batch_stride=20000 * 128)
+    assert _attend("lazyllm_op_cache_attention", many, _step(n_heads=256, q_len=64, max_len=100)) == B.LAZYLLM_EINVAL
     # sizes whose byte counts pass 32 bits
     long = _cache(batch=64, capacity=131072, batch_stride=1 << 30)
     assert size(long, 64, 64, 131072 - 64, 0, True) >= 64 * 64 * 64 * 131072 * 4
@@ -102,6 +107,16 @@ def test_eviction_refuses_bad_arguments():
     assert B.lazyllm_op_cache_evict_workspace_bytes(_cache(head_dim=96), 10) == 0
     assert B.lazyllm_op_cache_evict_workspace_bytes(_cache(batch=1, capacity=(1 << 24) + 1), 10) == 0
     assert B.lib().lazyllm_op_cache_evict(None, ONE, ONE, ONE, 5, 0, 0, ONE, ONE, ONE, None, None, ONE, 1 << 30, None) == B.LAZYLLM_EINVAL
+
+
+def test_prefix_of_another_shape_is_refused():
+    k = torch.zeros(3, 20, 2, 64, dtype=torch.bfloat16)
+    cache = B.make_kv_cache(k, torch.zeros_like(k))
+    p = torch.zeros(5, 2, 64, dtype=torch.bfloat16)
+    for bad_k, bad_v in ((p[:0], p[:0]), (p[:, :1], p[:, :1]), (p, p[:4]), (p[0], p[0]), (p.transpose(0, 1), p.transpose(0, 1)), (p[..., ::2], p[..., ::2])):
+        with pytest.raises(B.LazyLLMError) as e:
+            B.lazyllm_op_prefix_attention(cache, bad_k, bad_v, k, k, k, k, 2, 1, 10, k, k)
+        assert e.value.status == B.LAZYLLM_EINVAL
 
 
 def test_descriptor_of_caches():
