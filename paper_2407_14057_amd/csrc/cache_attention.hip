@@ -9,6 +9,8 @@
 // range of keys; the query rows of a K,V head are the (token, query head of the group) pairs of one request for a
 // range of its own cache, and those of ALL requests for a range of the prefix, which is therefore read once.
 // The partial results (output, maximum, sum) of the ranges are merged by a second launch.
+#include <type_traits>
+
 #include "common.h"
 
 
@@ -50,17 +52,22 @@ __device__ __forceinline__ uint32_t pack_halves(uint32_t hi, uint32_t lo, bool u
 
 }  // namespace
 
-// A wave takes 32 keys at a time straight from memory into MFMA operands (16x16x32, both products transposed so that a
-// lane owns a query column: S^T = K Q^T, O^T = V^T P^T), the four waves of a workgroup take turns over the range.
-//   K: lane (c = lane % 16, g = lane / 16) holds dimensions 32 s + 8 g .. + 7 of key c: the A operand as it lies.
-//   V: lane (c, g) holds dimensions HD/16 c .. of the eight keys that its S^T accumulators belong to (4 g + r of each
-//      block of 16), whole rows of 256 bytes per 16 lanes; pairs of keys are put together by v_perm.  Output tile i then
-//      has dimension HD/16 c + i in row c, and no value of P changes its lane.
+// A wave takes 32 keys at a time, the four waves of a workgroup in turn over the range; both products run on 16x16x32 MFMAs,
+// transposed so that a lane owns a query column: S^T = K Q^T, O^T = V^T P^T.
+//   K: row by row into 32 rows of LDS that are the wave's own (no barrier: the copies of the next step start when this
+//      step's operands have been read), read as operands: lane (c = lane % 16, g = lane / 16) takes dimensions
+//      32 s + 8 g .. + 7 of key c.  Straight into operand registers, 64 bytes of 16 rows a load, was level without and 10 %
+//      slower with non-temporal loads (113.7 against 101 us below).
+//   V: straight into registers.  Lane (c, g) holds dimensions HD/16 c .. of the eight keys that its S^T accumulators belong
+//      to (4 g + r of each block of 16), whole rows of 256 bytes per 16 lanes; pairs of keys are put together by v_perm.
+//      Output tile i then has dimension HD/16 c + i in row c, and no value of P changes its lane.
 // P goes into the second product as two bf16 terms (value and remainder): one alone would add an error as large as the
-// rounding of the output itself, and the matrix cores idle here anyway, the kernel is bound by reading K and V.
-// ONCE: no keys are read by more than one row block.  V then comes by non-temporal loads (8 requests of 1 - 8 k tokens 121
-// -> 113 us, a prefix of 8192 for 16 requests 41 -> 36; K, of whose cache lines a load takes half, loses by them: 124, 38).
-template <int HD, int T, bool ONCE>
+// rounding of the output itself, and the matrix cores idle here anyway, the kernel is bound by reading K and V (8 requests
+// of 1 - 8 k tokens, 32 heads: 554 MB in 101 us with the merge; 16 of 8000, 8 K,V heads: 524 MB in 113).
+// STREAM: non-temporal loads.  0: none, row blocks share what is read; 1: V (8 requests of 1 - 8 k tokens 121 us without,
+// 113 with, before K went through LDS); 2: K too, for more than the last-level cache can hold from one call to the next
+// (launch_cache_attention).
+template <int HD, int T, int STREAM>
 __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionArgs a) {
   constexpr int KS = HD / 32;          // k-steps of the first product
   constexpr int NT = HD / 16;          // tiles of 16 output dimensions = dimensions a lane holds of a V row
@@ -75,8 +82,8 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
   const int kvd = a.n_kv * HD;
 
   // The K,V head varies fastest: workgroups are dealt out to the XCDs in turn, so that ranges that a short request does
-  // not have leave all XCDs with less to do (parts fastest: 8 requests of 1 - 8 k tokens 165 us, now 127), and row
-  // blocks of one range share an L2.
+  // not have leave all XCDs with less to do (8 requests of 1 - 8 k tokens in 1024 workgroups: 165 us with the ranges
+  // fastest, 125 so), and row blocks of one range share an L2.
   int id = blockIdx.x;
   const int prefix_items = a.shared_tiles ? 0 : a.prefix_parts * a.n_kv * a.prefix_blocks;
   Item it;
@@ -165,30 +172,72 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
     for (int i = 0; i < NT; ++i) acc[t][i] = {0.f, 0.f, 0.f, 0.f};
   }
 
-  bf16x8_t kf[2][KS];
-  auto row = [&](const uint16_t* base, const uint16_t* behind, int key, bool tail) {
-    if (!tail || key < it.n) return base + key * it.stride;
+  // rows of a step that reaches beyond key n: the new tokens' (the prefix: its last one again, masked)
+  auto tail_row = [&](const uint16_t* base, const uint16_t* behind, int key) {
+    if (key < it.n) return base + key * it.stride;
     return behind + min(key - it.n, it.n_tail - 1) * it.tail_stride;
   };
-  auto load_k = [&](int k0) {
-    const bool tail = k0 + STEP > it.n;
+  // K of a step goes through 32 rows of LDS of this wave's own: copied row by row, read as operands
+  constexpr int CHK = HD / 8, ROWS = 64 / CHK;        // 16-byte chunks of a row, rows of a copy
+  constexpr int COPIES = STEP / ROWS;
+  char* mine = (char*)lds + wave * STEP * HD * 2;
+  auto swz = [](int r) { return CHK == 16 ? swz128(r) : swz64(r); };
+  uint32_t k_from[COPIES];                            // this lane's part of a copy's address, in bytes
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
-      const uint16_t* kp = row(it.k, it.k_tail, k0 + 16 * sub + c, tail) + 8 * g;
+  for (int u = 0; u < COPIES; ++u) {
+    const int r = u * ROWS + lane / CHK;
+    k_from[u] = (uint32_t)(lane / CHK) * (uint32_t)it.stride * 2u + ((lane % CHK) ^ swz(r)) * 16;
+  }
+  const uint32_t v_from = 4u * g * (uint32_t)it.stride * 2u + NT * c * 2;
+  auto copy_k = [&](int k0) {
+    if (k0 + STEP <= it.n) {
+      const char* base = (const char*)(it.k + k0 * it.stride);
 #pragma unroll
-      for (int s = 0; s < KS; ++s) kf[sub][s] = *(const bf16x8_t*)(kp + 32 * s);
+      for (int u = 0; u < COPIES; ++u)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base + u * ROWS * 2 * it.stride + k_from[u]),
+                                         (__attribute__((address_space(3))) void*)(mine + u * 1024), 16, 0, STREAM == 2 ? 2 : 0);
+    } else {
+#pragma unroll
+      for (int u = 0; u < COPIES; ++u) {
+        const int r = u * ROWS + lane / CHK;
+        g2l16(tail_row(it.k, it.k_tail, k0 + r) + ((lane % CHK) ^ swz(r)) * 8, mine + u * 1024);
+      }
     }
   };
+  // q is here before the first copy starts: waited for inside the loop, it would have every copy waited for
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int i = 0; i < KS; ++i) asm volatile("" : "+v"(qf[t][i]));
   int k0 = it.lo + STEP * wave;
-  if (k0 < it.hi) load_k(k0);
-  for (; k0 < it.hi; k0 += STEP * WAVES) {
-    const bool tail = k0 + STEP > it.n;
+  if (k0 < it.hi) copy_k(k0);
+  auto step = [&](auto reaches_beyond) {
+    constexpr bool tail = decltype(reaches_beyond)::value;
     uint32_t vf[8][VW];
+    const char* vbase = (const char*)(it.v + k0 * it.stride);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const words_t* vp = (const words_t*)(row(it.v, it.v_tail, k0 + 16 * (j >> 2) + 4 * g + (j & 3), tail) + NT * c);
-      *(words_t*)vf[j] = ONCE ? __builtin_nontemporal_load(vp) : *vp;
+      const words_t* vp;
+      if (tail) vp = (const words_t*)(tail_row(it.v, it.v_tail, k0 + 16 * (j >> 2) + 4 * g + (j & 3)) + NT * c);
+      else vp = (const words_t*)(vbase + (16 * (j >> 2) + (j & 3)) * 2 * it.stride + v_from);
+      *(words_t*)vf[j] = STREAM > 0 ? __builtin_nontemporal_load(vp) : *vp;
     }
+    // K has landed (the eight loads of V are behind it)
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8_t kf[2][KS];
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+        kf[sub][i] = *(const bf16x8_t*)(mine + (16 * sub + c) * HD * 2 + (((4 * i + g) ^ swz(16 * sub + c)) * 16));
+    // read: the next step's K may come
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if (k0 + STEP * WAVES < it.hi) copy_k(k0 + STEP * WAVES);
+    __builtin_amdgcn_sched_barrier(0);
     float s[T][8];                      // s[t][4 sub + r]: key k0 + 16 sub + 4 g + r, not scaled
 #pragma unroll
     for (int t = 0; t < T; ++t)
@@ -200,10 +249,6 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
 #pragma unroll
         for (int r = 0; r < 4; ++r) s[t][4 * sub + r] = s4[r];
       }
-    // the next step's K is on its way during the rest of this one
-    __builtin_amdgcn_sched_barrier(0);
-    if (k0 + STEP * WAVES < it.hi) load_k(k0 + STEP * WAVES);
-    __builtin_amdgcn_sched_barrier(0);
     uint4 p_hi[T], p_lo[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
@@ -258,7 +303,10 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
         acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, *(const bf16x8_t*)&p_lo[t], acc[t][i], 0, 0, 0);
       }
     }
-  }
+    k0 += STEP * WAVES;
+  };
+  while (k0 < it.hi && k0 + STEP <= it.n) step(std::false_type{});
+  while (k0 < it.hi) step(std::true_type{});
 
   // the new tokens of this range into the cache (nobody reads slots n and up from it in this launch)
   if (it.own && it.row0 == 0 && it.hi > it.n) {
@@ -273,6 +321,7 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
       a.pos[(size_t)b * a.capacity + first + threadIdx.x] = a.pos_new[b] + first - it.n + threadIdx.x;
   }
 
+  __syncthreads();                      // (K's rows are read: the waves' results go where they were)
   // the four waves, merged through LDS
 #pragma unroll
   for (int t = 0; t < T; ++t) {
@@ -665,16 +714,21 @@ __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttention
 // How a call is cut, measured (us):
 //  - the prefix through shared tiles where its work, query rows of a K,V head x keys x K,V heads x head_dim, is above
 //    2.5 G and there are 128 rows or more: below that the launch more costs more than the tiles save.  In units of 128 M
-//    (rows x keys, 8 K,V heads of 128), direct / shared: 256 x 4000 = 8.2: 23 / 30; 512 x 4000 = 16: 33 / 37;
-//    256 x 16000 = 33: 53 / 46; 1024 x 4000 = 33: 52 / 41; 2048 x 32000: 607 / 272; 32 heads, 64 x 16000 = 33: 76 / 79;
-//    4 heads of 64, 256 x 32000 = 16: 43 / 35, 512 x 4000 = 4: 18 / 24.
-//  - row tiles: one up to 16 rows, else two (a prefix of 3376 for 128 rows: one 21.7, two 18.2, four 22.4).
-//  - ranges of a cache: one request about 256 workgroups (30000 tokens, 8 K,V heads: 34.6 with 256, 38.5 with 512, 44 with
-//    1024), several up to 4096, because their lengths differ (eight of 1 - 8 k: 131 with 1024, 121 with 4096; 64 of up to
-//    2000: 56 / 40), but at least 256 keys and 48 per query row, since a range leaves a partial result of each row
-//    (16 requests of 5 tokens, 20 rows: ranges of 1024 keys 72, of 512 74, of 256 81).
-//  - ranges of the prefix: about 256 workgroups, at least 256 keys per row tile (128 rows, 3376 keys: 256 keys 19.5, 512
-//    18.5; 8 rows of 32 heads, 1000 keys: 20.5 / 22.6).
+//    (rows x keys, 8 K,V heads of 128), direct / shared: 256 x 4000 = 8.2: 23 / 30; 128 x 16000 = 16: 32 / 35; 512 x 4000 =
+//    16: 32 / 34; 128 x 32000 = 33: 62 / 54; 256 x 16000 = 33: 52 / 44; 1024 x 4000 = 33: 53 / 40; 2048 x 32000 = 524:
+//    597 / 254; 32 heads, 64 x 16000 = 33: 77 / 90; 4 heads of 64, 512 x 4000 = 4: 17 / 22, 256 x 32000 = 16: 43 / 30.
+//  - row tiles: one up to 16 rows, else two (a prefix of 3376 for 128 rows: 20.1 with one, 16.6 with two).
+//  - ranges of a cache: one request about 256 workgroups (30000 tokens, 8 K,V heads: 27 with 256, 30 with 512, 33 with
+//    1024), several up to 4096, because their lengths differ (eight of 1 - 8 k: 125 with 1024, 117 with 2048, 112 with
+//    4096, 111 with 8192; 64 of up to 2000: 51, 37, 36, 36), but at least 256 keys and 48 per query row, since a range
+//    leaves a partial result of each row (16 requests of 5 tokens, 20 rows: ranges of 1024 keys 68, of 512 70, of 256 80).
+//  - ranges of the prefix: about 256 workgroups, at least 256 keys per row tile (128 rows, 3376 keys: 256 keys 17.3, 512
+//    16.9, 1024 20.7; 8 rows of 32 heads, 1000 keys: 19, 21, 27).
+//  - K by non-temporal loads (V always, where no row blocks share them) from 400 MB of K and V on, by the bound that the host
+//    knows of the lengths: the last-level cache holds 256 MB, and what can be there from the call before is read from
+//    there.  K cached / streamed: 8 x 1 - 8 k tokens of 32 heads (1074 MB at most, 554 in fact) 108 / 101; 8 x 4000 (524) 100
+//    / 95; 16 x 8000 of 8 K,V heads (524) 116 / 113; 131 k (537) 115 / 112; 32 x 150 - 2100 (275, 86 in fact, three sets of
+//    caches in turn) 28 / 31; a prefix of 8192 of 32 heads and 16 x 50 - 500 (265, 166 in fact) 34.5 / 36.5.
 CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int head_dim, int q_len, int max_len,
                                         int prefix_len, bool weights) {
   CacheAttentionPlan p{};
@@ -698,6 +752,9 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
   cut((long long)max_len + q_len, (long long)batch * n_kv * p.own_blocks, batch == 1 ? 256 : 4096, least, p.own_range, p.own_parts);
   if (prefix_len > 0) cut(prefix_len, (long long)n_kv * p.prefix_blocks, 256, p.shared_tiles ? 256 : 256 * p.tiles, p.prefix_range,
                           p.prefix_parts);
+  const bool once = p.own_blocks == 1 && (p.shared_tiles || p.prefix_blocks <= 1);
+  const double keys = (double)batch * (max_len + q_len) + (p.shared_tiles ? 0 : prefix_len);
+  p.stream = !once ? 0 : keys * n_kv * head_dim * 4 >= 400e6 ? 2 : 1;
   const size_t all_rows = (size_t)batch * q_len * n_heads;
   const int parts = p.own_parts + p.prefix_parts;
   p.merge = parts == 1 ? 0 : parts <= 16 ? 1 : 2;
@@ -745,26 +802,28 @@ hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan
     else LZ_PATT(64);
 #undef LZ_PATT
   }
-  const bool once = p.own_blocks == 1 && (p.shared_tiles || p.prefix_blocks <= 1);
-#define LZ_CATT(HD, T, ONCE)                                                                                             \
+#define LZ_CATT(HD, T, STREAM)                                                                                     \
   do {                                                                                                             \
-    constexpr int LDS_BYTES = WAVES * 16 * T * (HD + 4) * 4 + WAVES * 16 * T * 8;                                  \
-    auto kern = cache_attention_kernel<HD, T, ONCE>;                                                                  \
+    constexpr int K_BYTES = WAVES * STEP * HD * 2, MERGE_BYTES = WAVES * 16 * T * (HD + 4) * 4 + WAVES * 16 * T * 8; \
+    constexpr int LDS_BYTES = K_BYTES > MERGE_BYTES ? K_BYTES : MERGE_BYTES;                                       \
+    auto kern = cache_attention_kernel<HD, T, STREAM>;                                                             \
     if (LDS_BYTES > 65536) {                                                                                       \
       hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES); \
       if (e != hipSuccess) return e;                                                                               \
     }                                                                                                              \
-    hipLaunchKernelGGL(kern, dim3(p.groups), dim3(64 * WAVES), LDS_BYTES, st, a);                           \
+    hipLaunchKernelGGL(kern, dim3(p.groups), dim3(64 * WAVES), LDS_BYTES, st, a);                                  \
   } while (0)
-  if (head_dim == 128) {
-    if (p.tiles == 1) LZ_CATT(128, 1, true);
-    else if (once) LZ_CATT(128, 2, true);
-    else LZ_CATT(128, 2, false);
-  } else {
-    if (p.tiles == 1) LZ_CATT(64, 1, true);
-    else if (once) LZ_CATT(64, 2, true);
-    else LZ_CATT(64, 2, false);
-  }
+#define LZ_CATT_HD(HD)                                                                                             \
+  do {                                                                                                             \
+    if (p.tiles == 1 && p.stream == 2) LZ_CATT(HD, 1, 2);                                                          \
+    else if (p.tiles == 1) LZ_CATT(HD, 1, 1);                                                                      \
+    else if (p.stream == 2) LZ_CATT(HD, 2, 2);                                                                     \
+    else if (p.stream == 1) LZ_CATT(HD, 2, 1);                                                                     \
+    else LZ_CATT(HD, 2, 0);                                                                                        \
+  } while (0)
+  if (head_dim == 128) LZ_CATT_HD(128);
+  else LZ_CATT_HD(64);
+#undef LZ_CATT_HD
 #undef LZ_CATT
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.merge_groups == 0) return e;

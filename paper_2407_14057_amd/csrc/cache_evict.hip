@@ -267,9 +267,9 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Caches of more slots: a workgroup per SEG slots, a launch per pass (one workgroup for 131000 slots took 176 us, nearly all
-// of it waiting for its own loads and LDS; these launches 35).  Per request the workspace holds the
-// segments' highest positions, the histograms, the bit masks and the new length.
+// Caches of more slots: a workgroup per SEG slots, a launch per pass (131000 slots, evicted to 16000: 62 us, of which 17 are
+// the list of moves by one workgroup; all by one workgroup: 176, nearly all of it waiting for its own loads and LDS).  Per
+// request the workspace holds the segments' highest positions, the histograms, the bit masks and what was found.
 constexpr int SEG = 8192, SEG_THREADS = 512, SEG_ITEMS = SEG / SEG_THREADS;
 
 namespace {
@@ -434,8 +434,8 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
     }
 }
 
-// The largest capacity that one workgroup selects from: up to here its launch is the quicker one (16000 slots: 28 us, of
-// which 19 are the selection, against some 30 for the launches of the long form).
+// The largest capacity that one workgroup selects from (its registers end here): so far its launch is the quicker form
+// (16000 slots, one request 26 us, the launches of the long form 39; eight requests 42 / 59).
 constexpr int SELECT_CAPACITY = 16384;
 
 static size_t move_bytes(int batch, int capacity, int budget) {
@@ -461,8 +461,9 @@ hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st) {
     hipLaunchKernelGGL(evict_long_pass_kernel<PASSES>, grid, dim3(SEG_THREADS), 0, st, a);
     hipLaunchKernelGGL(evict_long_moves_kernel, dim3(a.batch), dim3(1024), 0, st, a);
   } else {
-    // up to 256 KB of K and V to move for a request: by its selecting workgroup, a launch less
-    a.fused = a.max_moves <= FUSED_MOVES && (long long)a.max_moves * a.row_chunks * 32 <= 256 * 1024;
+    // up to 128 KB of K and V to move for a request: by its selecting workgroup, a launch less (32 caches, one row of 4 KB
+    // each: 9.2 us, with the launch 12.0; 8 caches, eight rows of 16 KB 11.8 / 12.4, sixteen rows 15.0 / 13.1)
+    a.fused = a.max_moves <= FUSED_MOVES && (long long)a.max_moves * a.row_chunks * 32 <= 128 * 1024;
     if (a.capacity <= 1024) hipLaunchKernelGGL((evict_select_kernel<256, 4>), dim3(a.batch), dim3(256), 0, st, a);
     else if (a.capacity <= 4096) hipLaunchKernelGGL((evict_select_kernel<512, 8>), dim3(a.batch), dim3(512), 0, st, a);
     else hipLaunchKernelGGL((evict_select_kernel<1024, 16>), dim3(a.batch), dim3(1024), 0, st, a);

@@ -363,6 +363,7 @@ struct CacheAttentionArgs {
 struct CacheAttentionPlan {
   int tiles;                           // 16-row tiles of query rows per work item
   int shared_tiles;                    // the prefix by prefix_attention_kernel
+  int stream;                          // non-temporal loads: 0 none, 1 of V, 2 of K and V
   int own_blocks, own_range, own_parts, prefix_blocks, prefix_range, prefix_parts;
   int merge;                           // 0: one part, no merge; else output rows merged by a wave (1) or a workgroup (2) each
   int z_ld;

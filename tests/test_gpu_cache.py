@@ -148,6 +148,15 @@ def test_attention_over_few_and_long_caches(heads, lengths, q_len):
     Step(HEADS[heads], lengths, q_len, seed=3).run_and_check()
 
 
+@pytest.mark.parametrize("heads,lengths,q_len", [("32/8x128", [50000, 700, -1], 1), ("32/8x128", [700, 33333], 5), ("4x64", [131000, 5, 64000, 129], 1),
+                                                 ("9/3x64", [140000, 1, 160001, 31], 7), ("2x128", [200000, 31], 1)])
+def test_attention_over_caches_beyond_the_last_level_cache(heads, lengths, q_len):
+    """K and V of 400 MB and more (by the bound on the lengths) come by non-temporal loads."""
+    s = Step(HEADS[heads], lengths, q_len, seed=5, max_len=max(max(lengths), 50000))
+    assert s.batch * s.max_len * s.kvh * s.hd * 4 >= 400e6
+    s.run_and_check()
+
+
 def test_attention_of_a_hundred_requests():
     rng = np.random.default_rng(5)
     Step((4, 2, 64), [int(x) for x in rng.integers(-1, 700, 130)], 2, seed=4).run_and_check()
