@@ -92,8 +92,11 @@ __device__ __forceinline__ int first_recent(int top, int recent) {
 // From the bit masks of the keys above the threshold (keep) and equal to it: which of the equal ones stay (the first
 // `need`), and the list of moves.  Holes are slots below the budget that lose their token, movers kept tokens from behind
 // it; as many of each, returned.  All threads of the workgroup; keep is complete on return, the lists after a barrier.
-template <int THREADS>
-__device__ __forceinline__ int resolve_moves(unsigned long long* keep, const unsigned long long* equal, int W, int kept, int need,
+// SPREAD: the words are dealt out again to write the lists, `equal` takes the counts (eight prompts of 1 - 8 k tokens to
+// 1100: 6 k cycles instead of the 13 k of a thread a word).  Not for small caches, where one barrier more costs as much as
+// it saves (a token of 2049: 9.7 us, 9.2 without), nor with the masks in memory (131000 slots: 85 us, 64 without).
+template <int THREADS, bool SPREAD>
+__device__ __forceinline__ int resolve_moves(unsigned long long* keep, unsigned long long* equal, int W, int kept, int need,
                                              bool all_equal, int32_t* hole_at, int32_t* mover_at, int2* part) {
   constexpr int WAVES = THREADS / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -139,20 +142,50 @@ __device__ __forceinline__ int resolve_moves(unsigned long long* keep, const uns
     }
     __syncthreads();
   }
-  int2 done = make_int2(0, 0);            // holes, movers
-  for (int w0 = 0; w0 < W; w0 += stride) {
-    const int at = w0 + own;
+  // holes and movers of a word
+  auto split = [&](int at, unsigned long long& hole, unsigned long long& mover) {
     const unsigned long long mine = at < W ? keep[at] : 0ull;
     const int below = min(max(kept - 64 * at, 0), 64);         // slots of this word below the budget
     const unsigned long long front = below == 64 ? ~0ull : (1ull << below) - 1ull;
-    unsigned long long hole = at < W ? ~mine & front : 0ull, mover = mine & ~front;
+    hole = at < W ? ~mine & front : 0ull;
+    mover = mine & ~front;
+  };
+  int2 done = make_int2(0, 0);            // holes, movers
+  for (int w0 = 0; w0 < W; w0 += stride) {
+    const int at = w0 + own;
+    unsigned long long hole, mover;
+    split(at, hole, mover);
     int2 total;
     const int2 first = over_words(__popcll(hole), __popcll(mover), total);
     int h = done.x + first.x, m = done.y + first.y;
     done = make_int2(done.x + total.x, done.y + total.y);
-    if (!one || wave == 0) {
+    if (SPREAD) {
+      if (at < W && (!one || wave == 0)) equal[at] = (unsigned long long)(unsigned)m << 32 | (unsigned)h;
+    } else if (!one || wave == 0) {
       for (; hole != 0ull; hole &= hole - 1ull) hole_at[h++] = 64 * at + __builtin_ctzll(hole);
       for (; mover != 0ull; mover &= mover - 1ull) mover_at[m++] = 64 * at + __builtin_ctzll(mover);
+    }
+  }
+  if (SPREAD) {
+    // the words dealt out to the waves, eight at a time; one word after the other, with a lane a slot
+    __syncthreads();
+    for (int w0 = wave * 8; w0 < W; w0 += WAVES * 8) {
+      const int at = w0 + (lane & 7);
+      unsigned long long hole, mover;
+      split(at, hole, mover);
+      const unsigned long long before = at < W ? equal[at] : 0ull;
+      for (unsigned long long busy = __ballot(lane < 8 && (hole | mover) != 0ull); busy != 0ull; busy &= busy - 1ull) {
+        const int l = __builtin_ctzll(busy);
+        auto emit = [&](unsigned long long bits, uint32_t from, int32_t* to) {
+          const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(bits >> 32), l);
+          const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)bits, l);
+          if (((lane < 32 ? lo : hi) >> (lane & 31)) & 1u)
+            to[__builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, (unsigned)__builtin_amdgcn_readlane((int)from, l)))] =
+                64 * (w0 + l) + lane;
+        };
+        emit(hole, (uint32_t)before, hole_at);
+        emit(mover, (uint32_t)(before >> 32), mover_at);
+      }
     }
   }
   return done.x;
@@ -248,7 +281,7 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
   __syncthreads();
   int32_t* hole_at = a.fused ? list[0] : a.moves + a.batch + (size_t)b * 2 * a.max_moves;
   int32_t* mover_at = a.fused ? list[1] : hole_at + a.max_moves;
-  const int holes = resolve_moves<THREADS>(keep, equal, W, kept, f.need, all_equal, hole_at, mover_at, part);
+  const int holes = resolve_moves<THREADS, (ITEMS > 8)>(keep, equal, W, kept, f.need, all_equal, hole_at, mover_at, part);
   if (threadIdx.x == 0 && !a.fused) a.moves[b] = holes;
   if (new_weight || new_pos || kept_from != nullptr)
     each([&](int u, int i) { if (i < kept && ((keep[i >> 6] >> (i & 63)) & 1ull)) stay(u, i); });
@@ -393,7 +426,7 @@ __global__ void __launch_bounds__(1024) evict_long_moves_kernel(EvictArgs a) {
   int holes = 0;
   if (n > a.budget) {
     int32_t* hole_at = a.moves + a.batch + (size_t)b * 2 * a.max_moves;
-    holes = resolve_moves<1024>(s.keep, s.equal, (n + 63) / 64, kept, s.found[0], s.found[0] == s.found[1], hole_at,
+    holes = resolve_moves<1024, false>(s.keep, s.equal, (n + 63) / 64, kept, s.found[0], s.found[0] == s.found[1], hole_at,
                                 hole_at + a.max_moves, part);
   }
   if (threadIdx.x == 0) {
@@ -404,7 +437,8 @@ __global__ void __launch_bounds__(1024) evict_long_moves_kernel(EvictArgs a) {
   }
 }
 
-// The tokens that move, a row of K and V at a time.  LONG: the tables of those that stay, unless a table is its own output,
+// The tokens that move, a row of K and V at a time, their old rows by non-temporal loads (eight prompts of 1 - 8 k tokens
+// brought down to 1100, 176 MB: 30 us; 38 by cached loads in a quarter of the workgroups).  LONG: the tables of those that stay, unless a table is its own output,
 // are written here too.
 template <bool LONG>
 __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
@@ -416,10 +450,20 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
   for (int i = blockIdx.x; i < count; i += gridDim.x) {
     const int to = hole_at[i], from = mover_at[i];
     const long long k_to = to * a.row_stride, k_from = from * a.row_stride;
-    for (int ch = threadIdx.x; ch < a.row_chunks; ch += 256) {
-      const uint4 x = *(const uint4*)(k + k_from + 8 * ch), y = *(const uint4*)(v + k_from + 8 * ch);
-      *(uint4*)(k + k_to + 8 * ch) = x;
-      *(uint4*)(v + k_to + 8 * ch) = y;
+    for (int ch = threadIdx.x; ch < a.row_chunks; ch += 512) {
+      const bool more = ch + 256 < a.row_chunks;
+      uint4 x2 = make_uint4(0u, 0u, 0u, 0u), y2 = x2;
+      const uint4 x = load_once((const uint4*)(k + k_from) + ch), y = load_once((const uint4*)(v + k_from) + ch);
+      if (more) {
+        x2 = load_once((const uint4*)(k + k_from) + ch + 256);
+        y2 = load_once((const uint4*)(v + k_from) + ch + 256);
+      }
+      ((uint4*)(k + k_to))[ch] = x;
+      ((uint4*)(v + k_to))[ch] = y;
+      if (more) {
+        ((uint4*)(k + k_to))[ch + 256] = x2;
+        ((uint4*)(v + k_to))[ch + 256] = y2;
+      }
     }
     if (threadIdx.x == 0) move_tables(a, b, to, from);
   }
@@ -471,7 +515,7 @@ hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st) {
   const bool one_workgroup = a.capacity <= SELECT_CAPACITY;
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || (one_workgroup && (a.max_moves == 0 || a.fused))) return e;
-  int groups = 2048 / a.batch;
+  int groups = 8192 / a.batch;
   if (groups < 16) groups = 16;
   const int useful = one_workgroup ? a.max_moves : a.max_moves + (a.capacity + 255) / 256;
   if (groups > useful) groups = useful;
