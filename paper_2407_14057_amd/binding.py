@@ -483,12 +483,13 @@ def lazyllm_op_cache_attention(cache, q, k_new, v_new, lengths, n_heads, q_len, 
 def lazyllm_op_prefix_attention(cache, prefix_k, prefix_v, q, k_new, v_new, lengths, n_heads, q_len, max_len, o, workspace,
                                 weight=None, weight_out=None, pos_new=None, pos=None, status=None, stream=None) -> None:
     """prefix_k, prefix_v: [prefix_len, n_kv_heads, head_dim], possibly strided from row to row."""
-    if (prefix_k.shape != prefix_v.shape or prefix_k.stride() != prefix_v.stride() or prefix_k.dim() != 3 or
-            prefix_k.shape[0] < 1 or prefix_k.shape[1:] != (cache.n_kv_heads, cache.head_dim) or not prefix_k[0].is_contiguous()):
+    shape, stride = prefix_k.shape, prefix_k.stride()
+    if (shape != prefix_v.shape or stride != prefix_v.stride() or len(shape) != 3 or shape[0] < 1 or
+            shape[1] != cache.n_kv_heads or shape[2] != cache.head_dim or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2])):
         raise LazyLLMError(LAZYLLM_EINVAL)
-    row = prefix_k.stride(0) if prefix_k.shape[0] > 1 else prefix_k[0].numel()
+    row = stride[0] if shape[0] > 1 else shape[1] * shape[2]
     s = lazyllm_step_attention(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(o), _ptr(lengths), n_heads, q_len, max_len,
-                               prefix_k.shape[0], prefix_k.data_ptr(), prefix_v.data_ptr(), row, _ptr(weight),
+                               shape[0], prefix_k.data_ptr(), prefix_v.data_ptr(), row, _ptr(weight),
                                _ptr(weight_out), _ptr(pos_new), _ptr(pos), _ptr(status))
     _check(lib().lazyllm_op_prefix_attention(C.byref(cache), C.byref(s), _ptr(workspace),
                                              workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
