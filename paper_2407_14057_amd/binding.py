@@ -82,6 +82,7 @@ class lazyllm_profile_record(C.Structure):
 class lazyllm_kv_cache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("batch_stride", C.c_int64), ("row_stride", C.c_int64),
                 ("batch", C.c_int32), ("capacity", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+    device = None                            # of the tensors that make_kv_cache was given
 
 
 class lazyllm_step_attention(C.Structure):
@@ -457,13 +458,26 @@ def lazyllm_op_lm_head(h_last, gain, w_lm, xf, logits, d, vocab, eps, stream=Non
 def make_kv_cache(k: torch.Tensor, v: torch.Tensor) -> lazyllm_kv_cache:
     """Descriptor of caches k, v [batch, capacity, n_kv_heads, head_dim] (bf16; strided views of one layout are
     fine as long as a row's [n_kv_heads, head_dim] is contiguous).  The tensors must outlive it."""
-    if k.shape != v.shape or k.stride() != v.stride() or k.dim() != 4 or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
+    if (k.shape != v.shape or k.stride() != v.stride() or k.dim() != 4 or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16 or
+            k.device != v.device):
         raise LazyLLMError(LAZYLLM_EINVAL)
     batch, capacity, heads, hd = k.shape
     if (hd > 1 and k.stride(3) != 1) or (heads > 1 and k.stride(2) != hd):
         raise LazyLLMError(LAZYLLM_EINVAL)
     row = k.stride(1) if capacity > 1 else heads * hd          # (the stride of a dimension of one means nothing)
-    return lazyllm_kv_cache(k.data_ptr(), v.data_ptr(), k.stride(0), row, batch, capacity, heads, hd)
+    cache = lazyllm_kv_cache(k.data_ptr(), v.data_ptr(), k.stride(0), row, batch, capacity, heads, hd)
+    cache.device = k.get_device()
+    return cache
+
+
+def _cache_stream(cache: lazyllm_kv_cache, workspace: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
+    """Stream of an operation on caches.  A kernel starts on the current device: caches, workspace or a stream of
+    another one (or in host memory) are refused."""
+    here = torch.cuda.current_device()
+    if (workspace.get_device() != here or (cache.device is not None and cache.device != here) or
+            (stream is not None and stream.device_index != here)):
+        raise LazyLLMError(LAZYLLM_EINVAL)
+    return torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream
 
 
 def lazyllm_op_cache_attention_workspace_bytes(cache: lazyllm_kv_cache, n_heads: int, q_len: int, max_len: int,
@@ -477,22 +491,23 @@ def lazyllm_op_cache_attention(cache, q, k_new, v_new, lengths, n_heads, q_len, 
     s = lazyllm_step_attention(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(o), _ptr(lengths), n_heads, q_len, max_len, 0, None,
                                None, 0, _ptr(weight), _ptr(weight_out), _ptr(pos_new), _ptr(pos), _ptr(status))
     _check(lib().lazyllm_op_cache_attention(C.byref(cache), C.byref(s), _ptr(workspace),
-                                            workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                            workspace.nbytes, _cache_stream(cache, workspace, stream)))
 
 
 def lazyllm_op_prefix_attention(cache, prefix_k, prefix_v, q, k_new, v_new, lengths, n_heads, q_len, max_len, o, workspace,
                                 weight=None, weight_out=None, pos_new=None, pos=None, status=None, stream=None) -> None:
     """prefix_k, prefix_v: [prefix_len, n_kv_heads, head_dim], possibly strided from row to row."""
     shape, stride = prefix_k.shape, prefix_k.stride()
-    if (shape != prefix_v.shape or stride != prefix_v.stride() or len(shape) != 3 or shape[0] < 1 or
-            shape[1] != cache.n_kv_heads or shape[2] != cache.head_dim or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2])):
+    if (prefix_k.dtype != torch.bfloat16 or prefix_v.dtype != torch.bfloat16 or shape != prefix_v.shape or
+            stride != prefix_v.stride() or len(shape) != 3 or shape[0] < 1 or shape[1] != cache.n_kv_heads or
+            shape[2] != cache.head_dim or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2])):
         raise LazyLLMError(LAZYLLM_EINVAL)
     row = stride[0] if shape[0] > 1 else shape[1] * shape[2]
     s = lazyllm_step_attention(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(o), _ptr(lengths), n_heads, q_len, max_len,
                                shape[0], prefix_k.data_ptr(), prefix_v.data_ptr(), row, _ptr(weight),
                                _ptr(weight_out), _ptr(pos_new), _ptr(pos), _ptr(status))
     _check(lib().lazyllm_op_prefix_attention(C.byref(cache), C.byref(s), _ptr(workspace),
-                                             workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                             workspace.nbytes, _cache_stream(cache, workspace, stream)))
 
 
 def lazyllm_op_cache_evict_workspace_bytes(cache: lazyllm_kv_cache, budget: int) -> int:
@@ -503,7 +518,7 @@ def lazyllm_op_cache_evict(cache, weight, pos, lengths, budget, sinks, recent, w
                            kept=None, status=None, stream=None) -> None:
     _check(lib().lazyllm_op_cache_evict(C.byref(cache), _ptr(weight), _ptr(pos), _ptr(lengths), budget, sinks, recent,
                                         _ptr(weight_out), _ptr(pos_out), _ptr(lengths_out), _ptr(kept), _ptr(status),
-                                        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                        _ptr(workspace), workspace.nbytes, _cache_stream(cache, workspace, stream)))
 
 
 # ---------------------------------------------------------------------------- decoding steps

@@ -132,3 +132,44 @@ def test_descriptor_of_caches():
         with pytest.raises(B.LazyLLMError) as e:
             B.make_kv_cache(bad_k, bad_v)
         assert e.value.status == B.LAZYLLM_EINVAL
+
+
+def test_prefix_of_another_type_is_refused():
+    k = torch.zeros(3, 20, 2, 64, dtype=torch.bfloat16)
+    cache = B.make_kv_cache(k, k.clone())
+    p = torch.zeros(5, 2, 64, dtype=torch.bfloat16)
+    for bad_k, bad_v in ((p.half(), p.half()), (p, p.float())):
+        with pytest.raises(B.LazyLLMError) as e:
+            B.lazyllm_op_prefix_attention(cache, bad_k, bad_v, k, k, k, k, 2, 1, 10, k, k)
+        assert e.value.status == B.LAZYLLM_EINVAL
+
+
+def test_what_is_not_on_the_current_device_is_refused(monkeypatch):
+    """Caches, workspace or stream of another device, or in host memory (-1); the library is not reached."""
+    class On:                                            # stands for a tensor or a stream of a device
+        def __init__(self, device):
+            self.device_index, self.cuda_stream = device, 77
+
+        def get_device(self):
+            return self.device_index
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    cache = _cache()
+    assert B._cache_stream(cache, On(1), On(1)) == 77                      # (a descriptor made by hand has no device)
+    cache.device = 1
+    assert B._cache_stream(cache, On(1), On(1)) == 77
+    for where, ws, stream in ((0, 1, 1), (-1, 1, 1), (1, 0, 1), (1, -1, 1), (1, 1, 0), (0, 0, 0)):
+        cache.device = where
+        with pytest.raises(B.LazyLLMError) as e:
+            B._cache_stream(cache, On(ws), On(stream))
+        assert e.value.status == B.LAZYLLM_EINVAL
+    k = torch.zeros(3, 20, 2, 64, dtype=torch.bfloat16)
+    p, table = torch.zeros(5, 2, 64, dtype=torch.bfloat16), torch.zeros(3, 20)
+    host = B.make_kv_cache(k, k.clone())
+    assert host.device == -1
+    for call in (lambda: B.lazyllm_op_cache_attention(host, k, k, k, table, 2, 1, 10, k, k),
+                 lambda: B.lazyllm_op_prefix_attention(host, p, p, k, k, k, table, 2, 1, 10, k, k),
+                 lambda: B.lazyllm_op_cache_evict(host, table, table, table, 5, 0, 0, table, table, table, k)):
+        with pytest.raises(B.LazyLLMError) as e:
+            call()
+        assert e.value.status == B.LAZYLLM_EINVAL
