@@ -547,7 +547,8 @@ typedef struct lazyllm_kv_cache {
  *   lengths   int32 [batch]: tokens in the cache before this step.  Negative: the request takes no part, its
  *             rows of o are set to zero and its cache and tables are left as they are.
  *   q_len     new tokens of every request, 1 .. 64.  max_len: the most that a length can be, at least 0, with
- *             max_len + q_len <= capacity; grids and workspace follow it.  A length beyond it counts as
+ *             max_len + q_len <= capacity; grids and workspace follow it, the work up to 256 requests the lengths
+ *             themselves.  A length beyond it counts as
  *             max_len and sets LAZYLLM_ST_BAD_CU in *status (int32, may be NULL; bits are only ever added).
  *   q         [batch, q_len, n_heads, head_dim], rotary applied; n_heads a multiple of n_kv_heads, at most 256.
  *   k_new,    [batch, q_len, n_kv_heads, head_dim]: K (rotary applied) and V of the new tokens; they are written to
@@ -565,7 +566,7 @@ typedef struct lazyllm_kv_cache {
  * values that some new token of a request sees must be finite; what lies elsewhere is of no account.
  * Sums and softmax statistics are fp32 and o is rounded once; a probability enters the product with V as two bf16
  * terms (value and remainder), against a prefix of many query rows as one.  The same call gives the same bits every
- * time; other lengths' bounds, another batch or a prefix can change the order of a row's sums. */
+ * time; other requests' lengths, another bound on them, another batch or a prefix can change the order of a row's sums. */
 typedef struct lazyllm_step_attention {
   const void *q, *k_new, *v_new;
   void* o;

@@ -9,6 +9,7 @@
 // range of keys; the query rows of a K,V head are the (token, query head of the group) pairs of one request for a
 // range of its own cache, and those of ALL requests for a range of the prefix, which is therefore read once.
 // The partial results (output, maximum, sum) of the ranges are merged by a second launch.
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -20,6 +21,10 @@ namespace {
 
 constexpr int STEP = 32;              // keys of a wave's step
 constexpr int WAVES = 4;
+constexpr int SPLIT_BATCH = 256;      // most requests whose ranges follow the lengths
+
+// Ranges are multiples of what the four waves take in turn.
+__host__ __device__ __forceinline__ int round_range(int keys) { return (keys + STEP * WAVES - 1) / (STEP * WAVES) * (STEP * WAVES); }
 
 // Row r of an item is token tok0 + r / group, query head kvh * group + r % group.
 struct Item {
@@ -34,6 +39,12 @@ struct Item {
 
 __device__ __forceinline__ int cached_tokens(const CacheAttentionArgs& a, int b) {
   return min(a.lengths[b], a.max_len);            // negative: the request takes no part
+}
+
+// parts that a request left, given its number of cached tokens
+__device__ __forceinline__ int parts_of(const CacheAttentionArgs& a, int b, int n) {
+  if (n < 0) return 0;
+  return a.prefix_parts + (a.own_split > 0 ? a.counts[b] : (n + a.q_len + a.own_range - 1) / a.own_range);
 }
 
 typedef short short4_t __attribute__((ext_vector_type(4)));
@@ -81,9 +92,8 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
   const int c = lane & 15, g = lane >> 4;
   const int kvd = a.n_kv * HD;
 
-  // The K,V head varies fastest: workgroups are dealt out to the XCDs in turn, so that ranges that a short request does
-  // not have leave all XCDs with less to do (8 requests of 1 - 8 k tokens in 1024 workgroups: 165 us with the ranges
-  // fastest, 125 so), and row blocks of one range share an L2.
+  // The K,V head varies fastest: workgroups are dealt out to the XCDs in turn, so that all of them get as much of every
+  // request, and row blocks of one range share an L2.
   int id = blockIdx.x;
   const int prefix_items = a.shared_tiles ? 0 : a.prefix_parts * a.n_kv * a.prefix_blocks;
   Item it;
@@ -97,12 +107,43 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
     it.row0 = id % blocks * 16 * T;
     id /= blocks;
   }
-  int b = 0;
-  if (it.own && a.batch > 1) {
+  int b = 0, part = id, own_range = a.own_range, own_parts = 0, given = 0;
+  if (it.own && a.own_split > 0) {
+    // Of all requests' keys every range gets about its share: a lane a request, 64 requests at a time.
+    int length[SPLIT_BATCH / 64], keys[SPLIT_BATCH / 64];
+    uint32_t total = 0;                                          // (below 2^31, as batch * capacity)
+#pragma unroll
+    for (int u = 0; u < SPLIT_BATCH / 64; ++u) length[u] = 64 * u + lane < a.batch ? a.lengths[64 * u + lane] : -1;
+#pragma unroll
+    for (int u = 0; u < SPLIT_BATCH / 64; ++u)
+      if (64 * u < a.batch) {
+        keys[u] = length[u] >= 0 ? min(length[u], a.max_len) + a.q_len : 0;
+        total += (uint32_t)__builtin_amdgcn_readlane(wave_scan(keys[u]), 63);
+      }
+    const int range = max(own_range, round_range((int)min((total + a.own_split - 1) / a.own_split, 1u << 30)));
+    int before = 0;                                              // parts of the 64s before
+    b = -1;
+#pragma unroll
+    for (int u = 0; u < SPLIT_BATCH / 64; ++u)
+      if (b < 0 && 64 * u < a.batch) {
+        const int parts = (keys[u] + range - 1) / range, upto = before + wave_scan(parts);
+        const int at = __popcll(__ballot(upto <= id));
+        before = __builtin_amdgcn_readlane(upto, 63);
+        if (at < 64) {
+          b = 64 * u + at;
+          given = __builtin_amdgcn_readlane(length[u], at);
+          part = id - __builtin_amdgcn_readlane(upto - parts, at);
+          // equal ranges of this request
+          const int mine = __builtin_amdgcn_readlane(keys[u], at), n_parts = __builtin_amdgcn_readlane(parts, at);
+          own_range = round_range((mine + n_parts - 1) / n_parts);
+          own_parts = (mine + own_range - 1) / own_range;
+        }
+      }
+    if (b < 0) return;                 // (more workgroups than parts)
+  } else if (it.own && a.batch > 1) {
     b = id % a.batch;
-    id /= a.batch;
+    part = id / a.batch;
   }
-  const int part = id;
   it.tok0 = b * a.q_len;
   it.n_rows = (it.own ? 1 : a.batch) * a.q_len * a.group;
 
@@ -133,7 +174,7 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
     it.hi = min(it.lo + a.prefix_range, a.prefix_len);
   } else {
     it.part = a.prefix_parts + part;
-    const int given = a.lengths[b];
+    if (a.own_split == 0) given = a.lengths[b];
     it.n = min(given, a.max_len);
     if (it.n < 0) {
       // no partial results: the output rows are zero (with more than one part the second launch clears them)
@@ -145,8 +186,10 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
         }
       return;
     }
-    if (part == 0 && it.kvh == 0 && it.row0 == 0 && threadIdx.x == 0 && a.status != nullptr && given > a.max_len)
-      atomicOr(a.status, ST_BAD_CU);
+    if (part == 0 && it.kvh == 0 && it.row0 == 0 && threadIdx.x == 0) {
+      if (a.status != nullptr && given > a.max_len) atomicOr(a.status, ST_BAD_CU);
+      if (a.own_split > 0) a.counts[b] = own_parts;
+    }
     it.stride = a.row_stride;
     it.k = a.k + b * a.batch_stride + it.kvh * HD;
     it.v = a.v + b * a.batch_stride + it.kvh * HD;
@@ -154,8 +197,8 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
     it.k_tail = a.k_new + ((size_t)it.tok0 * a.n_kv + it.kvh) * HD;
     it.v_tail = a.v_new + ((size_t)it.tok0 * a.n_kv + it.kvh) * HD;
     it.tail_stride = kvd;
-    it.lo = part * a.own_range;
-    it.hi = min(it.lo + a.own_range, it.n + a.q_len);
+    it.lo = part * own_range;
+    it.hi = min(it.lo + own_range, it.n + a.q_len);
   }
   if (it.lo >= it.hi) return;
   int last[T];                          // the last key that a query row sees
@@ -427,8 +470,7 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) 
       }
     };
     fetch(first);
-    const int n = cached_tokens(a, row / (a.q_len * a.n_heads));
-    const int parts = n < 0 ? 0 : a.prefix_parts + (n + a.q_len + a.own_range - 1) / a.own_range;
+    const int request = row / (a.q_len * a.n_heads), parts = parts_of(a, request, cached_tokens(a, request));
     const float2 ml = merged_stat(st, all_rows, parts, lane & 7);
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = 0.f;
@@ -461,7 +503,7 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) 
   const int n = cached_tokens(a, b);
   if (n < 0 || slot0 >= n + a.q_len) return;
   const int rows = a.q_len * a.n_heads, row0 = b * rows;
-  const int parts = a.prefix_parts + (n + a.q_len + a.own_range - 1) / a.own_range;
+  const int parts = parts_of(a, b, n);
   const bool mine = slot < n + a.q_len;
   const float before = wave == 0 && slot < n ? a.weight[(size_t)b * a.capacity + slot] : 0.f;
   const float* zp = a.z + (size_t)row0 * a.z_ld + min(slot, n + a.q_len - 1);
@@ -718,10 +760,15 @@ __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttention
 //    16: 32 / 34; 128 x 32000 = 33: 62 / 54; 256 x 16000 = 33: 52 / 44; 1024 x 4000 = 33: 53 / 40; 2048 x 32000 = 524:
 //    597 / 254; 32 heads, 64 x 16000 = 33: 77 / 90; 4 heads of 64, 512 x 4000 = 4: 17 / 22, 256 x 32000 = 16: 43 / 30.
 //  - row tiles: one up to 16 rows, else two (a prefix of 3376 for 128 rows: 20.1 with one, 16.6 with two).
-//  - ranges of a cache: one request about 256 workgroups (30000 tokens, 8 K,V heads: 27 with 256, 30 with 512, 33 with
-//    1024), several up to 4096, because their lengths differ (eight of 1 - 8 k: 125 with 1024, 117 with 2048, 112 with
-//    4096, 111 with 8192; 64 of up to 2000: 51, 37, 36, 36), but at least 256 keys and 48 per query row, since a range
-//    leaves a partial result of each row (16 requests of 5 tokens, 20 rows: ranges of 1024 keys 68, of 512 70, of 256 80).
+//  - ranges of the caches, up to 256 requests: by the lengths, which the host does not know; every workgroup finds its range
+//    from all of them.  About 256 ranges x K,V heads a request, at most 2048 (one row tile) or 512 (two: as many workgroups
+//    as run at once).  By max_len / by the lengths: 32 x 150 - 2100 tokens 28.4 / 25.5; 16 x 0.7 - 8 k, 20 rows 69.1 / 60.3;
+//    64 x 5 - 2000 39.6 / 34.1; 2 x 20 and 64 k 109 / 89; 4 x 4 - 30 k, 20 rows 90 / 76; one of 4000, the bound itself, 11.8 / 12.3.
+//    Ranges in all 512 / 1024 / 2048 / 4096: 8 x 1 - 8 k of 32 heads 112 / 104 / 101 / 99; 16 x 8000 109 / 108 / 109 / 117; 64 x 0.5 -
+//    2 k 76 / 73 / 72 / 72; two row tiles, 4 x 4 - 30 k: 76 / 82 / 93; one request of 30000, 32 rows, from 256 on: 49 / 60 / 65 / 75.
+//    At least 256 keys, 512 with more than 8 rows of a K,V head, since a range leaves a partial result of each row (16 x 0.7 -
+//    8 k, 20 rows: 256 keys 63.5, 512 60.3, 768 60.4; 32 x 150 - 2100, 4 rows: 25.3, 25.1, 28.1; one of 4000: 12.5, 14.3, 17.2).
+//    More requests: equal ranges by max_len.
 //  - ranges of the prefix: about 256 workgroups, at least 256 keys per row tile (128 rows, 3376 keys: 256 keys 17.3, 512
 //    16.9, 1024 20.7; 8 rows of 32 heads, 1000 keys: 19, 21, 27).
 //  - K by non-temporal loads (V always, where no row blocks share them) from 400 MB of K and V on, by the bound that the host
@@ -743,13 +790,18 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
     const long long want = groups > items ? groups / items : 1;
     long long r = (keys + want - 1) / want;
     if (r < least) r = least;
-    r = (r + 127) / 128 * 128;
-    range = (int)r;
+    r = range = round_range((int)r);
     parts = (int)((keys + r - 1) / r);
   };
-  long long least = 48 * (own_rows < rows ? own_rows : rows);
-  if (least < 256) least = 256;
-  cut((long long)max_len + q_len, (long long)batch * n_kv * p.own_blocks, batch == 1 ? 256 : 4096, least, p.own_range, p.own_parts);
+  const long long least = own_rows > 8 ? 512 : 256, most_keys = (long long)max_len + q_len, per_range = (long long)n_kv * p.own_blocks;
+  const long long split = std::min(256ll * batch, p.tiles == 1 ? 2048ll : 512ll) / per_range;
+  if (batch <= SPLIT_BATCH && split > 1 && most_keys > least) {
+    p.own_split = (int)split;
+    p.own_range = (int)least;
+    p.own_parts = (int)std::min((most_keys + least - 1) / least, split);
+  } else {
+    cut(most_keys, batch * per_range, 4096, least, p.own_range, p.own_parts);
+  }
   if (prefix_len > 0) cut(prefix_len, (long long)n_kv * p.prefix_blocks, 256, p.shared_tiles ? 256 : 256 * p.tiles, p.prefix_range,
                           p.prefix_parts);
   const bool once = p.own_blocks == 1 && (p.shared_tiles || p.prefix_blocks <= 1);
@@ -763,8 +815,10 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
   p.part_bytes = p.merge ? up(all_rows * parts * head_dim * 4) : 0;
   p.stat_bytes = p.merge || weights ? up(all_rows * parts * 8) : 0;
   p.z_bytes = weights ? up(all_rows * p.z_ld * 4) : 0;
+  p.count_bytes = p.own_split ? up(batch * 4) : 0;
   const size_t prefix_items = (size_t)p.prefix_parts * n_kv * p.prefix_blocks;
-  const size_t items = (size_t)batch * n_kv * p.own_blocks * p.own_parts + (p.shared_tiles ? 0 : prefix_items);
+  const size_t own_items = (size_t)per_range * std::min((size_t)batch * p.own_parts, p.own_split ? (size_t)(p.own_split + batch) : SIZE_MAX);
+  const size_t items = own_items + (p.shared_tiles ? 0 : prefix_items);
   const size_t merge_items = (p.merge == 0 ? 0 : p.merge == 1 ? (all_rows + WAVES - 1) / WAVES : all_rows) +
                              (weights ? (size_t)batch * ((max_len + q_len + 63) / 64) : 0);
   const size_t most = 0xffffffffull / 512;           // threads of a launch are counted in 32 bits
@@ -778,7 +832,7 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
 hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan& p, int head_dim, void* workspace, hipStream_t st) {
   a.group = a.n_heads / a.n_kv;
   a.scale_log2e = 1.4426950408889634f / sqrtf((float)head_dim);
-  a.own_blocks = p.own_blocks; a.own_range = p.own_range; a.own_parts = p.own_parts;
+  a.own_blocks = p.own_blocks; a.own_range = p.own_range; a.own_split = p.own_split; a.own_parts = p.own_parts;
   a.prefix_blocks = p.prefix_blocks; a.prefix_range = p.prefix_range; a.prefix_parts = p.prefix_parts;
   a.shared_tiles = p.shared_tiles;
   a.merge = p.merge;
@@ -787,6 +841,7 @@ hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan
   a.part = p.part_bytes ? (float*)ws : nullptr;
   a.stat = p.stat_bytes ? (float2*)(ws + p.part_bytes) : nullptr;
   a.z = p.z_bytes ? (float*)(ws + p.part_bytes + p.stat_bytes) : nullptr;
+  a.counts = p.count_bytes ? (int32_t*)(ws + p.part_bytes + p.stat_bytes + p.z_bytes) : nullptr;
   if (p.shared_tiles) {
 #define LZ_PATT(HD)                                                                                                \
   do {                                                                                                             \

@@ -24,17 +24,6 @@ __device__ __forceinline__ uint32_t eviction_key(float w, int pos, int sinks, bo
   return pos < sinks || (any_recent && pos >= recent_from) ? 0xffffffffu : key;
 }
 
-// inclusive sum over the lanes of a wave (DPP: rows of 16, then the rows' totals handed on)
-__device__ __forceinline__ int wave_scan(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);    // row_shr:1
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);    // row_bcast:15 into rows 1 and 3
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);    // row_bcast:31 into rows 2 and 3
-  return v;
-}
-
 // Adds every lane with `on` to its bin; where all of them have the same bin (ties), at once: LDS atomics on one address
 // take a turn per lane.
 __device__ __forceinline__ void count_bins(int* hist, uint32_t bin, bool on) {

@@ -337,6 +337,17 @@ int decode_key_splits(int M, int n_keys, int n_heads, int head_dim, size_t split
 // (the ticket counters at its end must be zero before the first attention launch: launch_gen_embed)
 
 // ---- a batch's K,V caches (cache_attention.hip, cache_evict.hip) --------------------------
+// inclusive sum over the lanes of a wave (DPP: rows of 16, then the rows' totals handed on)
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);    // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);    // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);    // row_bcast:31 into rows 2 and 3
+  return v;
+}
+
 // Strides in elements; slot s of request b starts at b * batch_stride + s * row_stride.
 struct CacheAttentionArgs {
   uint16_t *k, *v;
@@ -354,8 +365,9 @@ struct CacheAttentionArgs {
   int32_t* pos;
   int32_t* status;
   // filled in by the launcher
-  int group, own_blocks, own_range, own_parts, prefix_blocks, prefix_range, prefix_parts, shared_tiles, merge, z_ld;
+  int group, own_blocks, own_range, own_split, own_parts, prefix_blocks, prefix_range, prefix_parts, shared_tiles, merge, z_ld;
   float scale_log2e;
+  int32_t* counts;                     // [batch] parts of a request, if own_split is not 0
   float* part;                         // [parts][rows][head_dim], rows = batch * q_len * n_heads
   float2* stat;                        // [parts][rows] (maximum, sum), base 2
   float* z;                            // [rows][z_ld] base-2 logits against the own cache
@@ -365,12 +377,13 @@ struct CacheAttentionPlan {
   int shared_tiles;                    // the prefix by prefix_attention_kernel
   int stream;                          // non-temporal loads: 0 none, 1 of V, 2 of K and V
   int own_blocks, own_range, own_parts, prefix_blocks, prefix_range, prefix_parts;
+  int own_split;                       // 0: ranges of own_range; else of own_range or more, such that all requests have about so many
   int merge;                           // 0: one part, no merge; else output rows merged by a wave (1) or a workgroup (2) each
   int z_ld;
   unsigned prefix_groups, groups, merge_groups;   // workgroups of the three launches; 0: no such launch
   bool fits;                           // ... are what a launch can have
-  size_t part_bytes, stat_bytes, z_bytes;
-  size_t bytes() const { return part_bytes + stat_bytes + z_bytes; }
+  size_t part_bytes, stat_bytes, z_bytes, count_bytes;
+  size_t bytes() const { return part_bytes + stat_bytes + z_bytes + count_bytes; }
 };
 CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int head_dim, int q_len, int max_len,
                                         int prefix_len, bool weights);

@@ -162,6 +162,27 @@ def test_attention_of_a_hundred_requests():
     Step((4, 2, 64), [int(x) for x in rng.integers(-1, 700, 130)], 2, seed=4).run_and_check()
 
 
+@pytest.mark.parametrize("batch", [1, 2, 63, 64, 65, 128, 200, 256, 257])
+@pytest.mark.parametrize("q_len", [1, 9])
+def test_lengths_far_below_their_bound(batch, q_len):
+    """The caches are cut by the lengths that are there: few long ones, many short ones, idle requests, one beyond the bound."""
+    rng = np.random.default_rng(batch)
+    lengths = [int(x) for x in np.exp(rng.uniform(0, 5, batch))]
+    for at, n in ((0, 2100), (5, 0), (62, -1), (63, 1303), (64, -3), (127, 257), (128, 2502), (199, -1), (255, 511), (256, 900)):
+        if at < batch:
+            lengths[at] = n
+    s = Step((4, 2, 64), [min(n, 2500) for n in lengths], q_len, seed=31, max_len=2500)        # (rows beyond the bound are NaN)
+    s.len_dev.copy_(torch.tensor(lengths))
+    s.run_and_check()
+    assert (int(s.status.item()) != 0) == (batch > 128)
+    o, weight = s.o.clone(), s.weight_out.clone()
+    s.run()
+    assert torch.equal(s.o, o) and torch.equal(s.weight_out[:, :1], weight[:, :1])
+    if batch <= 2:                        # the bound alone changes where a row of ranges ends, not what is computed
+        for max_len in (2200, 5000, 70000):
+            Step((4, 2, 64), lengths, q_len, seed=31, max_len=max_len, slack=0).run_and_check()
+
+
 def test_without_weights_and_alone():
     """One request that one workgroup per head serves, and the same as part of a batch, without the weights."""
     for lengths in ([90], [90, 400, -1]):
