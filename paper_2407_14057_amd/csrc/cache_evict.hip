@@ -8,7 +8,7 @@
 //
 // One workgroup per request selects (latency bound: a few KB of tables, some ten barriers), a second launch moves the
 // rows of K and V at the rate of a copy; where the caches have room for a few evictions only, the selecting workgroup
-// moves them itself.
+// moves them itself.  Where only a few tokens leave, as in a cache that is full, they are found directly.
 #include "common.h"
 
 namespace lz {
@@ -16,12 +16,26 @@ namespace lz {
 namespace {
 
 constexpr int FUSED_MOVES = 512;                    // most rows that a selecting workgroup moves itself
+constexpr int FEW = 8;                              // most tokens that are looked for one after the other
+
+constexpr uint32_t PROTECTED = 0xfffffffeu, NOBODY = 0xffffffffu;
 
 // sorts like the weight; above every weight: a protected token; lowest: NaN
 __device__ __forceinline__ uint32_t eviction_key(float w, int pos, int sinks, bool any_recent, int recent_from) {
   const uint32_t u = __float_as_uint(w + 0.f);               // -0 counts as 0
   const uint32_t key = w != w ? 0u : u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
-  return pos < sinks || (any_recent && pos >= recent_from) ? 0xffffffffu : key;
+  return pos < sinks || (any_recent && pos >= recent_from) ? PROTECTED : key;
+}
+
+// lowest of the lanes' values, in every lane
+__device__ __forceinline__ uint32_t wave_lowest(uint32_t v) {
+  v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(-1, (int)v, 0x111, 0xf, 0xf, false));      // (the steps of wave_scan)
+  v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(-1, (int)v, 0x112, 0xf, 0xf, false));
+  v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(-1, (int)v, 0x114, 0xf, 0xf, false));
+  v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(-1, (int)v, 0x118, 0xf, 0xf, false));
+  v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(-1, (int)v, 0x142, 0xa, 0xf, false));
+  v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(-1, (int)v, 0x143, 0xc, 0xf, false));
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 // Adds every lane with `on` to its bin; where all of them have the same bin (ties), at once: LDS atomics on one address
@@ -83,7 +97,7 @@ __device__ __forceinline__ int first_recent(int top, int recent) {
 // it; as many of each, returned.  All threads of the workgroup; keep is complete on return, the lists after a barrier.
 // SPREAD: the words are dealt out again to write the lists, `equal` takes the counts (eight prompts of 1 - 8 k tokens to
 // 1100: 6 k cycles instead of the 13 k of a thread a word).  Not for small caches, where one barrier more costs as much as
-// it saves (a token of 2049: 9.7 us, 9.2 without), nor with the masks in memory (131000 slots: 85 us, 64 without).
+// it saves (2049 slots: 9.7 us, 9.2 without), nor with the masks in memory (131000 slots: 85 us, 64 without).
 template <int THREADS, bool SPREAD>
 __device__ __forceinline__ int resolve_moves(unsigned long long* keep, unsigned long long* equal, int W, int kept, int need,
                                              bool all_equal, int32_t* hole_at, int32_t* mover_at, int2* part) {
@@ -197,6 +211,7 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
   __shared__ __attribute__((aligned(16))) int hist[PASSES][BINS];
   __shared__ int2 part[WAVES];
   __shared__ int list[2][FUSED_MOVES];
+  __shared__ uint2 low[2][WAVES];
   const int b = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float* weight = a.weight + (size_t)b * a.capacity;
   const int32_t* pos = a.pos + (size_t)b * a.capacity;
@@ -246,42 +261,83 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
   }
   const int recent_from = first_recent(top, a.recent);
   each([&](int u, int) { keys[u] = eviction_key(w[u], p[u], a.sinks, a.recent > 0, recent_from); });
-  Found f;
-  f.need = kept;
+  int holes;
+  const int leave = n - kept;
+  if (leave <= FEW) {
+    // A full cache that gives a token up for every new one: the lowest keys, of equal ones the higher slot, are found one
+    // after the other, and their rows moved by this workgroup (32 caches, of 2049 tokens one: 6.7 us, by the histograms 9.3;
+    // of 2056 eight: 9.3, 9.8; 16 caches, one of 8192: 8.4, 17.7).
+    int gone = INT32_MAX;                // the slot that was found j-th, in lane j
+    uint32_t behind = 0u;                // those from the budget on, as bits
+    auto all = [&](auto f) {             // (no branch an item, as `each` has, where there is so little to do)
 #pragma unroll
-  for (int pass = 0; pass < PASSES; ++pass) {
-    each([&](int u, int i) { count_bins(hist[pass], pass_bin(keys[u], pass), i < n && (keys[u] & f.mask) == f.prefix); });
-    __syncthreads();
-    next_digit(f, hist[pass], pass);
-  }
-
-  // kept set as a bit mask: keys above the threshold, and the first `need` equal to it
-  const int W = (n + 63) / 64;
-  const bool all_equal = f.need == f.same;
-  each([&](int u, int i) {
-    const unsigned long long hi = __ballot(i < n && (all_equal ? keys[u] >= f.prefix : keys[u] > f.prefix));
-    const unsigned long long eq = __ballot(i < n && keys[u] == f.prefix);
-    const int at = u * WAVES + wave;
-    if (lane == 0 && at < W) {
-      keep[at] = hi;
-      equal[at] = eq;
+      for (int u = 0; u < ITEMS; ++u) f(u, u * THREADS + (int)threadIdx.x);
+    };
+    all([&](int u, int i) { keys[u] = i < n ? keys[u] : NOBODY; });
+    for (int j = 0; j < leave; ++j) {
+      // (slots as their complement)
+      uint32_t key = NOBODY, from = NOBODY;
+      all([&](int u, int) { key = min(key, keys[u]); });
+      key = wave_lowest(key);
+      all([&](int u, int i) { from = min(from, keys[u] == key ? ~(uint32_t)i : NOBODY); });
+      from = wave_lowest(from);
+      if (lane == 0) low[j & 1][wave] = make_uint2(key, from);
+      __syncthreads();
+      const uint2 said = lane < WAVES ? low[j & 1][lane] : make_uint2(NOBODY, NOBODY);
+      key = wave_lowest(said.x);
+      const int slot = (int)~wave_lowest(said.x == key ? said.y : NOBODY);
+      all([&](int u, int i) { keys[u] = i == slot ? NOBODY : keys[u]; });
+      if (lane == j) gone = slot;
+      if (slot >= kept) behind |= 1u << (slot - kept);
     }
-  });
-  __syncthreads();
-  int32_t* hole_at = a.fused ? list[0] : a.moves + a.batch + (size_t)b * 2 * a.max_moves;
-  int32_t* mover_at = a.fused ? list[1] : hole_at + a.max_moves;
-  const int holes = resolve_moves<THREADS, (ITEMS > 8)>(keep, equal, W, kept, f.need, all_equal, hole_at, mover_at, part);
-  if (threadIdx.x == 0 && !a.fused) a.moves[b] = holes;
-  if (new_weight || new_pos || kept_from != nullptr)
-    each([&](int u, int i) { if (i < kept && ((keep[i >> 6] >> (i & 63)) & 1ull)) stay(u, i); });
-  if (!a.fused) return;
-  __syncthreads();                        // the lists are read by other threads of this workgroup
-  for (int i = threadIdx.x; i < holes; i += THREADS) move_tables(a, b, hole_at[i], mover_at[i]);
+    holes = __popcll(__ballot(gone < kept));
+    int rank = 0;
+    for (int j = 0; j < leave; ++j) rank += __builtin_amdgcn_readlane(gone, j) < gone;
+    if (wave == 0 && gone < kept) list[0][rank] = gone;
+    if (wave == 0 && lane < leave && !((behind >> lane) & 1u)) list[1][__popc(~behind & ((1u << lane) - 1u))] = kept + lane;
+    if (new_weight || new_pos || kept_from != nullptr)
+      each([&](int u, int i) { if (i < kept && keys[u] != NOBODY) stay(u, i); });
+    if (threadIdx.x == 0 && !a.fused) a.moves[b] = 0;
+  } else {
+    Found f;
+    f.need = kept;
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+      each([&](int u, int i) { count_bins(hist[pass], pass_bin(keys[u], pass), i < n && (keys[u] & f.mask) == f.prefix); });
+      __syncthreads();
+      next_digit(f, hist[pass], pass);
+    }
+
+    // kept set as a bit mask: keys above the threshold, and the first `need` equal to it
+    const int W = (n + 63) / 64;
+    const bool all_equal = f.need == f.same;
+    each([&](int u, int i) {
+      const unsigned long long hi = __ballot(i < n && (all_equal ? keys[u] >= f.prefix : keys[u] > f.prefix));
+      const unsigned long long eq = __ballot(i < n && keys[u] == f.prefix);
+      const int at = u * WAVES + wave;
+      if (lane == 0 && at < W) {
+        keep[at] = hi;
+        equal[at] = eq;
+      }
+    });
+    __syncthreads();
+    int32_t* hole_at = a.fused ? list[0] : a.moves + a.batch + (size_t)b * 2 * a.max_moves;
+    int32_t* mover_at = a.fused ? list[1] : hole_at + a.max_moves;
+    holes = resolve_moves<THREADS, (ITEMS > 8)>(keep, equal, W, kept, f.need, all_equal, hole_at, mover_at, part);
+    if (new_weight || new_pos || kept_from != nullptr)
+      each([&](int u, int i) { if (i < kept && ((keep[i >> 6] >> (i & 63)) & 1ull)) stay(u, i); });
+    if (!a.fused) {
+      if (threadIdx.x == 0) a.moves[b] = holes;
+      return;
+    }
+  }
+  __syncthreads();                       // the lists are read by other threads
+  for (int i = threadIdx.x; i < holes; i += THREADS) move_tables(a, b, list[0][i], list[1][i]);
   uint16_t* k = a.k + b * a.batch_stride;
   uint16_t* v = a.v + b * a.batch_stride;
   for (int i = threadIdx.x; i < holes * a.row_chunks; i += THREADS) {
     const int row = i / a.row_chunks, ch = i % a.row_chunks * 8;
-    const long long to = hole_at[row] * a.row_stride + ch, from = mover_at[row] * a.row_stride + ch;
+    const long long to = list[0][row] * a.row_stride + ch, from = list[1][row] * a.row_stride + ch;
     const uint4 x = *(const uint4*)(k + from), y = *(const uint4*)(v + from);
     *(uint4*)(k + to) = x;
     *(uint4*)(v + to) = y;
@@ -494,8 +550,9 @@ hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st) {
     hipLaunchKernelGGL(evict_long_pass_kernel<PASSES>, grid, dim3(SEG_THREADS), 0, st, a);
     hipLaunchKernelGGL(evict_long_moves_kernel, dim3(a.batch), dim3(1024), 0, st, a);
   } else {
-    // up to 128 KB of K and V to move for a request: by its selecting workgroup, a launch less (32 caches, one row of 4 KB
-    // each: 9.2 us, with the launch 12.0; 8 caches, eight rows of 16 KB 11.8 / 12.4, sixteen rows 15.0 / 13.1)
+    // up to 128 KB of K and V to move for a request: by its selecting workgroup, a launch less (32 caches, 32 rows of 4 KB each:
+    // 13.4 us, with the launch 14.6; 64 rows 19.1 / 17.7; 8 caches, 16 rows of 16 KB 14.5 / 13.4; 32 caches, 128 rows of 1 KB 14.3 /
+    // 17.2)
     a.fused = a.max_moves <= FUSED_MOVES && (long long)a.max_moves * a.row_chunks * 32 <= 128 * 1024;
     if (a.capacity <= 1024) hipLaunchKernelGGL((evict_select_kernel<256, 4>), dim3(a.batch), dim3(256), 0, st, a);
     else if (a.capacity <= 4096) hipLaunchKernelGGL((evict_select_kernel<512, 8>), dim3(a.batch), dim3(512), 0, st, a);

@@ -533,6 +533,17 @@ def test_eviction_of_one_request(n, budget):
 
 
 @pytest.mark.parametrize("values", ["tied", "equal", "odd", "spread"])
+@pytest.mark.parametrize("budget,slack", [(1, 12), (9, 12), (300, 11), (300, 700), (1500, 11), (4090, 500), (9000, 11), (17000, 11)])
+def test_eviction_of_a_few_tokens(values, budget, slack):
+    """Up to eleven tokens leave, from caches with and without room for many more."""
+    lengths = [budget + 3, budget, -1, budget + 1, 0] + [budget + j for j in range(2, 12)]
+    c = Cache(lengths, budget + slack, heads=(1, 64) if slack < 100 else (4, 128), seed=budget + slack, values=values)
+    c.run_and_check(budget, min(4, budget // 3), budget // 2, in_place=budget % 2 == 0)
+    c.len_dev.copy_(torch.tensor(lengths))
+    c.run_and_check(budget, 0, 0, in_place=budget % 2 == 1)
+
+
+@pytest.mark.parametrize("values", ["tied", "equal", "odd", "spread"])
 def test_eviction_from_caches_that_several_workgroups_select_from(values):
     lengths = [16385, 0, -1, 7, 8192, 8193, 300, 16500, 16384, 12000]
     Cache(lengths, 16500, seed=11, values=values).run_and_check(250, 4, 60)
