@@ -441,20 +441,24 @@ __device__ __forceinline__ float2 merged_stat(const float2* __restrict__ st, siz
 }
 
 // Merges the partial results and adds the weights.  The first workgroups take an output row each (its parts dealt out to
-// the four waves) or, with few parts, one row a wave; the others 128 slots of a request each: a lane two slots, every wave a
-// quarter of its rows, in a fixed order.  (64 slots: 60.5 us for 16 requests of 0.7 - 8 k, five tokens each, where this takes
-// 59.4, and 108 for 106.4 on 16 of 8000; logits fetched ahead of the statistics, or eight or sixteen waves: no faster.)
-template <int HD>
-__global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) {
+// the waves) or, with few parts, one row a wave; the others 128 slots of a request each: a lane two slots, every wave a
+// share of its rows, in a fixed order.  (64 slots: 60.5 us for 16 requests of 0.7 - 8 k, five tokens each, where this took
+// 59.4, and 108 for 106.4 on 16 of 8000.)  MW waves: 16 where a slot gets the weights of 64 rows or more, which they read
+// sooner, 4 elsewhere, where the workgroups are many and short.  4 / 16 waves: 8 tokens of one request of 1900 24.4 / 18.3 us,
+// 17 requests of 2 - 63 20.0 / 14.5, five of 16 of 0.7 - 8 k 58.1 / 57.0, two (64 rows) of 44 of 80 - 640 24.8 / 24.3; one token (32 rows) of
+// one of 131071 109 / 114, of 32 of 150 - 2100 25.6 / 26.5.
+template <int HD, int MW>
+__global__ void __launch_bounds__(64 * MW) cache_merge_kernel(CacheAttentionArgs a) {
   constexpr int E = HD / 64;           // output dimensions of a lane
+  constexpr int RB = MW == 16 ? 4 : 8; // rows whose logits a wave reads at a time
   __shared__ float2 stats[256];
-  __shared__ float sums[WAVES][HD], slot_sums[WAVES][SLOTS][64];
+  __shared__ float sums[MW][HD], slot_sums[MW][SLOTS][64];
   const int all_rows = a.batch * a.q_len * a.n_heads;
-  const int merge_groups = a.merge == 0 ? 0 : a.merge == 1 ? (all_rows + WAVES - 1) / WAVES : all_rows;
+  const int merge_groups = a.merge == 0 ? 0 : a.merge == 1 ? (all_rows + MW - 1) / MW : all_rows;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if ((int)blockIdx.x < merge_groups) {
-    const int row = a.merge == 1 ? blockIdx.x * WAVES + wave : blockIdx.x;
-    const int first = a.merge == 1 ? 0 : wave, step = a.merge == 1 ? 1 : WAVES;
+    const int row = a.merge == 1 ? blockIdx.x * MW + wave : blockIdx.x;
+    const int first = a.merge == 1 ? 0 : wave, step = a.merge == 1 ? 1 : MW;
     if (row >= all_rows) return;       // (of whole waves, and only where no barrier follows)
     const float2* st = a.stat + row;
     const float* src = a.part + (size_t)row * HD + E * lane;
@@ -492,7 +496,9 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) 
       __syncthreads();
       if (wave != 0) return;
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = ((sums[0][E * lane + e] + sums[1][E * lane + e]) + sums[2][E * lane + e]) + sums[3][E * lane + e];
+      for (int e = 0; e < E; ++e)
+#pragma unroll
+        for (int u = 1; u < MW; ++u) x[e] += sums[u][E * lane + e];
     }
     const float inv = parts == 0 ? 0.f : 1.0f / ml.y;
     if (E == 2) ((uint32_t*)(a.o + (size_t)row * HD))[lane] = pack_bf16(x[0] * inv, x[E - 1] * inv);
@@ -514,27 +520,24 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) 
   for (int base = 0; base < rows; base += 256) {
     const int count = min(256, rows - base);
     __syncthreads();
-    for (int r = threadIdx.x >> 3; r < count; r += 32) {
+    for (int r = threadIdx.x >> 3; r < count; r += 8 * MW) {
       const float2 ml = merged_stat(a.stat + row0 + base + r, all_rows, parts, threadIdx.x & 7);
       if ((threadIdx.x & 7) == 0) stats[r] = make_float2(ml.x, 1.0f / ml.y);
     }
     __syncthreads();
-    // every wave a quarter of the rows
-    const int quarter = (count + WAVES - 1) / WAVES, end = min(count, (wave + 1) * quarter);
-    int r = wave * quarter;
-    for (; r + 8 <= end; r += 8) {
-      slots_t z[8];
+    // every wave its share of the rows
+    const int share = (count + MW - 1) / MW, end = min(count, (wave + 1) * share);
+    for (int r = wave * share; r < end; r += RB) {
+      slots_t z[RB];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) z[u] = *(const slots_t*)(zp + (size_t)(base + r + u) * a.z_ld);
+      for (int u = 0; u < RB; ++u) z[u] = *(const slots_t*)(zp + (size_t)(base + min(r + u, end - 1)) * a.z_ld);
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+      for (int u = 0; u < RB; ++u) {
+        const float2 ml = stats[min(r + u, end - 1)];
+        const float inv = r + u < end ? ml.y : 0.f;
 #pragma unroll
-        for (int e = 0; e < SLOTS; ++e) sum[e] += __builtin_amdgcn_exp2f(z[u][e] - stats[r + u].x) * stats[r + u].y;
-    }
-    for (; r < end; ++r) {
-      const slots_t z = *(const slots_t*)(zp + (size_t)(base + r) * a.z_ld);
-#pragma unroll
-      for (int e = 0; e < SLOTS; ++e) sum[e] += __builtin_amdgcn_exp2f(z[e] - stats[r].x) * stats[r].y;
+        for (int e = 0; e < SLOTS; ++e) sum[e] += __builtin_amdgcn_exp2f(z[u][e] - ml.x) * inv;
+      }
     }
   }
 #pragma unroll
@@ -542,9 +545,12 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttentionArgs a) 
   __syncthreads();
   if (wave < SLOTS) {
     const int s = slot + wave;
-    if (s < n + a.q_len)
-      a.weight_out[(size_t)b * a.capacity + s] = (s < n ? a.weight[(size_t)b * a.capacity + s] : 0.f) +
-          (((slot_sums[0][wave][lane] + slot_sums[1][wave][lane]) + slot_sums[2][wave][lane]) + slot_sums[3][wave][lane]) / (float)a.n_heads;
+    if (s < n + a.q_len) {
+      float x = slot_sums[0][wave][lane];
+#pragma unroll
+      for (int u = 1; u < MW; ++u) x += slot_sums[u][wave][lane];
+      a.weight_out[(size_t)b * a.capacity + s] = (s < n ? a.weight[(size_t)b * a.capacity + s] : 0.f) + x / (float)a.n_heads;
+    }
   }
 }
 
@@ -823,6 +829,7 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
   const size_t all_rows = (size_t)batch * q_len * n_heads;
   const int parts = p.own_parts + p.prefix_parts;
   p.merge = parts == 1 ? 0 : parts <= 16 ? 1 : 2;
+  p.merge_waves = weights && q_len * n_heads >= 64 ? 16 : 4;
   p.z_ld = (max_len + q_len + STEP - 1) / STEP * STEP;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   p.part_bytes = p.merge ? up(all_rows * parts * head_dim * 4) : 0;
@@ -832,9 +839,9 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
   const size_t prefix_items = (size_t)p.prefix_parts * n_kv * p.prefix_blocks;
   const size_t own_items = (size_t)per_range * std::min((size_t)batch * p.own_parts, p.own_split ? (size_t)(p.own_split + batch) : SIZE_MAX);
   const size_t items = own_items + (p.shared_tiles ? 0 : prefix_items);
-  const size_t merge_items = (p.merge == 0 ? 0 : p.merge == 1 ? (all_rows + WAVES - 1) / WAVES : all_rows) +
+  const size_t merge_items = (p.merge == 0 ? 0 : p.merge == 1 ? (all_rows + p.merge_waves - 1) / p.merge_waves : all_rows) +
                              (weights ? (size_t)batch * ((max_len + q_len + 64 * SLOTS - 1) / (64 * SLOTS)) : 0);
-  const size_t most = 0xffffffffull / 512;           // threads of a launch are counted in 32 bits
+  const size_t most = 0xffffffffull / 1024;          // threads of a launch are counted in 32 bits
   p.fits = prefix_items <= most && items <= most && merge_items <= most && all_rows <= 0x7fffffff;
   p.prefix_groups = p.shared_tiles ? (unsigned)prefix_items : 0;
   p.groups = (unsigned)items;
@@ -895,8 +902,15 @@ hipError_t launch_cache_attention(CacheAttentionArgs a, const CacheAttentionPlan
 #undef LZ_CATT
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.merge_groups == 0) return e;
-  if (head_dim == 128) hipLaunchKernelGGL(cache_merge_kernel<128>, dim3(p.merge_groups), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(cache_merge_kernel<64>, dim3(p.merge_groups), dim3(256), 0, st, a);
+#define LZ_MERGE(HD, MW) hipLaunchKernelGGL((cache_merge_kernel<HD, MW>), dim3(p.merge_groups), dim3(64 * MW), 0, st, a)
+  if (p.merge_waves == 16) {
+    if (head_dim == 128) LZ_MERGE(128, 16);
+    else LZ_MERGE(64, 16);
+  } else {
+    if (head_dim == 128) LZ_MERGE(128, 4);
+    else LZ_MERGE(64, 4);
+  }
+#undef LZ_MERGE
   return hipGetLastError();
 }
 

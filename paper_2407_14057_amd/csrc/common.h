@@ -379,6 +379,7 @@ struct CacheAttentionPlan {
   int own_blocks, own_range, own_parts, prefix_blocks, prefix_range, prefix_parts;
   int own_split;                       // 0: ranges of own_range; else of own_range or more, such that all requests have about so many
   int merge;                           // 0: one part, no merge; else output rows merged by a wave (1) or a workgroup (2) each
+  int merge_waves;                     // of a workgroup of that launch
   int z_ld;
   unsigned prefix_groups, groups, merge_groups;   // workgroups of the three launches; 0: no such launch
   bool fits;                           // ... are what a launch can have
