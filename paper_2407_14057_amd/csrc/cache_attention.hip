@@ -788,6 +788,9 @@ __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttention
 //    At least 256 keys, 512 with more than 8 rows of a K,V head, since a range leaves a partial result of each row (16 x 0.7 -
 //    8 k, 20 rows: 256 keys 63.5, 512 60.3, 768 60.4; 32 x 150 - 2100, 4 rows: 25.3, 25.1, 28.1; one of 4000: 12.5, 14.3, 17.2).
 //    More requests: equal ranges by max_len.
+//  - an output row merged by a wave up to 16 parts, or 64 where there are 256 rows, else by a workgroup.  Wave / workgroup: 8
+//    requests of 2 - 16 k, five tokens, 1280 rows of up to 32 parts 65.5 / 74.5; 4 of 4 - 30 k, 640 rows 72.9 / 77.8; 128 rows behind a
+//    prefix of 25000, 33 parts 28.0 / 25.6; one of 131071, 32 rows of 32 106.9 / 105.0; by their number, 16 x 0.7 - 8 k of 16 56.6 / 69.4.
 //  - ranges of the prefix: about 256 workgroups, at least 256 keys per row tile (128 rows, 3376 keys: 256 keys 17.3, 512
 //    16.9, 1024 20.7; 8 rows of 32 heads, 1000 keys: 19, 21, 27).
 //  - K by non-temporal loads (V always, where no row blocks share them) from 400 MB of K and V on, by the bound that the host
@@ -828,7 +831,7 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
   p.stream = !once ? 0 : keys * n_kv * head_dim * 4 >= 400e6 ? 2 : 1;
   const size_t all_rows = (size_t)batch * q_len * n_heads;
   const int parts = p.own_parts + p.prefix_parts;
-  p.merge = parts == 1 ? 0 : parts <= 16 ? 1 : 2;
+  p.merge = parts == 1 ? 0 : parts <= 16 || (parts <= 64 && all_rows >= 256) ? 1 : 2;
   p.merge_waves = weights && q_len * n_heads >= 64 ? 16 : 4;
   p.z_ld = (max_len + q_len + STEP - 1) / STEP * STEP;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
