@@ -97,7 +97,7 @@ __device__ __forceinline__ int first_recent(int top, int recent) {
 // it; as many of each, returned.  All threads of the workgroup; keep is complete on return, the lists after a barrier.
 // SPREAD: the words are dealt out again to write the lists, `equal` takes the counts (eight prompts of 1 - 8 k tokens to
 // 1100: 6 k cycles instead of the 13 k of a thread a word).  Not for small caches, where one barrier more costs as much as
-// it saves (2049 slots: 9.7 us, 9.2 without), nor with the masks in memory (131000 slots: 85 us, 64 without).
+// it saves (2049 slots: 9.7 us, 9.2 without).
 template <int THREADS, bool SPREAD>
 __device__ __forceinline__ int resolve_moves(unsigned long long* keep, unsigned long long* equal, int W, int kept, int need,
                                              bool all_equal, int32_t* hole_at, int32_t* mover_at, int2* part) {
@@ -345,37 +345,53 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Caches of more slots: a workgroup per SEG slots, a launch per pass (131000 slots, evicted to 16000: 62 us, of which 17 are
-// the list of moves by one workgroup; all by one workgroup: 176, nearly all of it waiting for its own loads and LDS).  Per
-// request the workspace holds the segments' highest positions, the histograms, the bit masks and what was found.
-constexpr int SEG = 8192, SEG_THREADS = 512, SEG_ITEMS = SEG / SEG_THREADS;
+// Caches of more slots: a workgroup per SEG slots, a launch per pass (131000 slots brought down to 16000, 8 K,V heads: 48 us, 24 of
+// them the moves; in segments of 8192 slots and with the list of moves by one workgroup 72; all by one workgroup 176, nearly all
+// of it waiting for its own loads and LDS).  Segments are cut at the budget, so that one has either holes or movers.  Per request the workspace holds the segments' highest positions, the
+// histograms, the bit masks, how many bits those have, and what was found.
+constexpr int SEG = 2048, SEG_THREADS = 512, SEG_ITEMS = SEG / SEG_THREADS, SEG_WORDS = SEG / 64;
 
 namespace {
 
 struct LongState {                       // of one request, in the workspace
   int32_t *top, *hist, *found;           // found: duplicates of the threshold to keep, all of them, tokens kept
+  int2* counts;                          // of a segment: keys above the threshold (all that stay, if all duplicates do), equal to it
   unsigned long long *keep, *equal;
 };
-__host__ __device__ inline size_t long_state_bytes(int capacity) {
-  const size_t segs = (capacity + SEG - 1) / SEG;
-  return PASSES * BINS * 4 + segs * (SEG / 64) * 16 + ((segs + 3) * 4 + 255) / 256 * 256;
+// segments up to the budget
+__host__ __device__ inline int front_segs(int capacity, int budget) { return ((budget < capacity ? budget : capacity) + SEG - 1) / SEG; }
+__host__ __device__ inline int long_segs(int capacity, int budget) {
+  return front_segs(capacity, budget) + (budget < capacity ? (capacity - budget + SEG - 1) / SEG : 0);
+}
+__host__ __device__ inline size_t long_state_bytes(int capacity, int budget) {
+  const size_t segs = long_segs(capacity, budget);
+  return PASSES * BINS * 4 + segs * SEG_WORDS * 16 + (segs * 12 + 12 + 255) / 256 * 256;
 }
 __device__ __forceinline__ LongState long_state(const EvictArgs& a, int b) {
-  const size_t segs = (a.capacity + SEG - 1) / SEG;
-  char* at = (char*)a.long_state + b * long_state_bytes(a.capacity);
+  const size_t segs = long_segs(a.capacity, a.budget);
+  char* at = (char*)a.long_state + b * long_state_bytes(a.capacity, a.budget);
   LongState s;
   s.hist = (int32_t*)at;
   s.keep = (unsigned long long*)(at + PASSES * BINS * 4);
-  s.equal = s.keep + segs * (SEG / 64);
-  s.top = (int32_t*)(s.equal + segs * (SEG / 64));
+  s.equal = s.keep + segs * SEG_WORDS;
+  s.counts = (int2*)(s.equal + segs * SEG_WORDS);
+  s.top = (int32_t*)(s.counts + segs);
   s.found = s.top + segs;
   return s;
 }
+// First slot of a segment, and the slot behind its last one of a request of n tokens.
+struct Range {
+  int lo, hi;
+};
+__device__ __forceinline__ Range seg_range(const EvictArgs& a, int seg, int n) {
+  const int front = front_segs(a.capacity, a.budget), lo = seg < front ? seg * SEG : a.budget + (seg - front) * SEG;
+  return {lo, min(min(lo + SEG, seg < front ? a.budget : n), n)};
+}
 // Highest position of a request, from its segments'; all threads of a wave together.
-__device__ __forceinline__ int highest(const LongState& s, int n) {
+__device__ __forceinline__ int highest(const LongState& s, int segs) {
   const int lane = threadIdx.x & 63;
   int top = INT32_MIN;
-  for (int i = lane; i * SEG < n; i += 64) top = max(top, s.top[i]);
+  for (int i = lane; i < segs; i += 64) top = max(top, s.top[i]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
   return top;
@@ -386,7 +402,8 @@ __device__ __forceinline__ int highest(const LongState& s, int n) {
 // Highest position of a segment; the histograms are cleared.
 __global__ void __launch_bounds__(SEG_THREADS) evict_long_top_kernel(EvictArgs a) {
   __shared__ int part[SEG_THREADS / 64];
-  const int b = blockIdx.y, seg = blockIdx.x, n = min(a.lengths[b], a.capacity);
+  const int b = blockIdx.y, seg = blockIdx.x;
+  const Range r = seg_range(a, seg, min(a.lengths[b], a.capacity));
   const LongState s = long_state(a, b);
   for (int i = seg * SEG_THREADS + threadIdx.x; i < PASSES * BINS / 4; i += gridDim.x * SEG_THREADS)
     ((int4*)s.hist)[i] = make_int4(0, 0, 0, 0);
@@ -394,8 +411,8 @@ __global__ void __launch_bounds__(SEG_THREADS) evict_long_top_kernel(EvictArgs a
   int top = INT32_MIN;
 #pragma unroll
   for (int u = 0; u < SEG_ITEMS; ++u) {
-    const int i = seg * SEG + u * SEG_THREADS + threadIdx.x;
-    top = max(top, i < n ? pos[i] : INT32_MIN);
+    const int i = r.lo + u * SEG_THREADS + threadIdx.x;
+    top = max(top, i < r.hi ? pos[i] : INT32_MIN);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
@@ -411,8 +428,10 @@ __global__ void __launch_bounds__(SEG_THREADS) evict_long_top_kernel(EvictArgs a
 template <int PASS>
 __global__ void __launch_bounds__(SEG_THREADS) evict_long_pass_kernel(EvictArgs a) {
   __shared__ __attribute__((aligned(16))) int hist[BINS];
+  __shared__ int2 part[SEG_THREADS / 64];
   const int b = blockIdx.y, seg = blockIdx.x, n = min(a.lengths[b], a.capacity);
-  if (n <= a.budget || seg * SEG >= n) return;
+  const Range r = seg_range(a, seg, n);
+  if (n <= a.budget || r.lo >= r.hi) return;
   const LongState s = long_state(a, b);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float* weight = a.weight + (size_t)b * a.capacity;
@@ -421,7 +440,7 @@ __global__ void __launch_bounds__(SEG_THREADS) evict_long_pass_kernel(EvictArgs 
   int p[SEG_ITEMS];
 #pragma unroll
   for (int u = 0; u < SEG_ITEMS; ++u) {
-    const int i = min(seg * SEG + u * SEG_THREADS + (int)threadIdx.x, n - 1);
+    const int i = min(r.lo + u * SEG_THREADS + (int)threadIdx.x, r.hi - 1);
     w[u] = weight[i];
     p[u] = pos[i];
   }
@@ -429,62 +448,114 @@ __global__ void __launch_bounds__(SEG_THREADS) evict_long_pass_kernel(EvictArgs 
     for (int i = threadIdx.x; i < BINS / 4; i += SEG_THREADS) ((int4*)hist)[i] = make_int4(0, 0, 0, 0);
     __syncthreads();
   }
-  const int recent_from = first_recent(highest(s, n), a.recent);
+  const int recent_from = first_recent(highest(s, gridDim.x), a.recent);
   Found f;
   f.need = a.budget;
 #pragma unroll
   for (int pass = 0; pass < PASS; ++pass) next_digit(f, s.hist + pass * BINS, pass);
+  int2 count = make_int2(0, 0);
 #pragma unroll
   for (int u = 0; u < SEG_ITEMS; ++u) {
-    const int i = seg * SEG + u * SEG_THREADS + threadIdx.x;
+    const int i = r.lo + u * SEG_THREADS + threadIdx.x;
     const uint32_t key = eviction_key(w[u], p[u], a.sinks, a.recent > 0, recent_from);
     if (PASS < PASSES) {
-      count_bins(hist, pass_bin(key, PASS), i < n && (key & f.mask) == f.prefix);
+      count_bins(hist, pass_bin(key, PASS), i < r.hi && (key & f.mask) == f.prefix);
     } else {
-      const unsigned long long hi = __ballot(i < n && (f.need == f.same ? key >= f.prefix : key > f.prefix));
-      const unsigned long long eq = __ballot(i < n && key == f.prefix);
+      const unsigned long long hi = __ballot(i < r.hi && (f.need == f.same ? key >= f.prefix : key > f.prefix));
+      const unsigned long long eq = __ballot(i < r.hi && key == f.prefix);
+      count = make_int2(count.x + __popcll(hi), count.y + __popcll(eq));
       if (lane == 0) {
-        const int at = seg * (SEG / 64) + u * (SEG_THREADS / 64) + wave;
+        const int at = seg * SEG_WORDS + u * (SEG_THREADS / 64) + wave;
         s.keep[at] = hi;
         s.equal[at] = eq;
       }
     }
   }
-  if (PASS == PASSES && seg == 0 && threadIdx.x == 0) {
-    s.found[0] = f.need;
-    s.found[1] = f.same;
-  }
   if (PASS < PASSES) {
     __syncthreads();
     for (int i = threadIdx.x; i < pass_bins(PASS); i += SEG_THREADS)
       if (hist[i] != 0) atomicAdd(&s.hist[PASS * BINS + i], hist[i]);
+  } else {
+    if (lane == 0) part[wave] = count;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int v = 1; v < SEG_THREADS / 64; ++v) count = make_int2(count.x + part[v].x, count.y + part[v].y);
+      s.counts[seg] = count;
+      if (seg == 0) {
+        s.found[0] = f.need;
+        s.found[1] = f.same;
+      }
+    }
   }
 }
 
-// A request's moves, and its new length.
-__global__ void __launch_bounds__(1024) evict_long_moves_kernel(EvictArgs a) {
-  __shared__ int2 part[16];
-  const int b = blockIdx.x;
+// A segment's holes or movers, and which of its duplicates of the threshold stay (the first of the request's); by the first
+// one also how many moves there are.  The new length is written by the launch behind: others read the old one here.
+__global__ void __launch_bounds__(256) evict_long_moves_kernel(EvictArgs a) {
+  const int b = blockIdx.y, seg = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const LongState s = long_state(a, b);
-  const int given = a.lengths[b], n = min(given, a.capacity), kept = min(n, a.budget);
-  __syncthreads();                       // every thread has read the length, which may be overwritten now
-  int holes = 0;
-  if (n > a.budget) {
-    int32_t* hole_at = a.moves + a.batch + (size_t)b * 2 * a.max_moves;
-    holes = resolve_moves<1024, false>(s.keep, s.equal, (n + 63) / 64, kept, s.found[0], s.found[0] == s.found[1], hole_at,
-                                hole_at + a.max_moves, part);
-  }
-  if (threadIdx.x == 0) {
-    a.moves[b] = holes;
-    s.found[2] = kept;
-    a.lengths_out[b] = kept;
+  const int given = a.lengths[b], n = min(given, a.capacity), front = front_segs(a.capacity, a.budget);
+  if (seg == 0 && threadIdx.x == 0) {
+    s.found[2] = min(n, a.budget);
+    if (n <= a.budget) a.moves[b] = 0;
     if (given > a.capacity && a.status != nullptr) atomicOr(a.status, ST_BAD_CU);
   }
+  const Range r = seg_range(a, seg, n);
+  if (n <= a.budget || r.lo >= r.hi) return;
+  const int need = s.found[0] == s.found[1] ? 0 : s.found[0];
+  // sums over the segments before this one: duplicates, holes, movers; a lane a segment, every wave for itself
+  int equals = 0, holes = 0, movers = 0, mine = 0, left = 0;
+  for (int t0 = 0; t0 < (int)gridDim.x; t0 += 64) {
+    const int t = t0 + lane;
+    const Range q = seg_range(a, t, n);
+    const bool live = t < (int)gridDim.x && q.lo < q.hi;
+    const int2 count = live ? s.counts[t] : make_int2(0, 0);
+    const int eq = wave_scan(count.y), before = equals + eq - count.y;
+    const int stay = count.x + min(max(need - before, 0), count.y);
+    const int hole = live && t < front ? q.hi - q.lo - stay : 0, mover = live && t >= front ? stay : 0;
+    const int h = wave_scan(hole), m = wave_scan(mover);
+    if (seg >= t0 && seg < t0 + 64) {
+      left = need - __builtin_amdgcn_readlane(before, seg - t0);
+      mine = __builtin_amdgcn_readlane(seg < front ? holes + h - hole : movers + m - mover, seg - t0);
+    }
+    equals += __builtin_amdgcn_readlane(eq, 63);
+    holes += __builtin_amdgcn_readlane(h, 63);
+    movers += __builtin_amdgcn_readlane(m, 63);
+  }
+  if (seg == 0 && threadIdx.x == 0) a.moves[b] = holes;
+  // a lane a word of the masks (a wave that comes after the first one's store finds the same bits again)
+  unsigned long long keep = lane < SEG_WORDS ? s.keep[seg * SEG_WORDS + lane] : 0ull;
+  unsigned long long eq = lane < SEG_WORDS ? s.equal[seg * SEG_WORDS + lane] : 0ull;
+  const int equal_here = __popcll(eq);
+  left -= wave_scan(equal_here) - equal_here;
+  if (left >= equal_here) keep |= eq;
+  else
+    for (; left > 0; --left) {
+      keep |= eq & (~eq + 1ull);
+      eq &= eq - 1ull;
+    }
+  if (wave == 0 && lane < SEG_WORDS) s.keep[seg * SEG_WORDS + lane] = keep;
+  const int size = min(max(r.hi - r.lo - 64 * lane, 0), 64);
+  const unsigned long long bits = seg < front ? ~keep & (size == 64 ? ~0ull : (1ull << size) - 1ull) : keep;
+  const int from = mine + wave_scan(__popcll(bits)) - __popcll(bits);
+  int32_t* to = a.moves + a.batch + (size_t)b * 2 * a.max_moves + (seg < front ? 0 : a.max_moves);
+  // the words dealt out to the waves, with a lane a slot
+#pragma unroll
+  for (int u = 0; u < SEG_WORDS / 4; ++u) {
+    const int l = wave * (SEG_WORDS / 4) + u;
+    const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(bits >> 32), l);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)bits, l);
+    if (((lane < 32 ? lo : hi) >> (lane & 31)) & 1u)
+      to[__builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, (unsigned)__builtin_amdgcn_readlane(from, l)))] = r.lo + 64 * l + lane;
+  }
 }
 
-// The tokens that move, a row of K and V at a time, their old rows by non-temporal loads (eight prompts of 1 - 8 k tokens
-// brought down to 1100, 176 MB: 30 us; 38 by cached loads in a quarter of the workgroups).  LONG: the tables of those that stay, unless a table is its own output,
-// are written here too.
+__host__ __device__ inline int rows_at_once(int row_chunks) { return row_chunks < 256 ? 256 / row_chunks : 1; }
+
+// The tokens that move, a row of K and V at a time, narrow ones several, their old rows by non-temporal loads (eight prompts of
+// 1 - 8 k tokens brought down to 1100, 176 MB: 30 us; 38 by cached loads in a quarter of the workgroups; 32 caches of 8000, rows of
+// 512 bytes, to 1000: 29.8 us in all, one row at a time 44.7).  LONG: the tables of those that stay, unless a table is its own
+// output, and the new length are written here too.
 template <bool LONG>
 __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
   const int b = blockIdx.y, count = a.moves[b];
@@ -492,10 +563,13 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
   const int32_t* mover_at = hole_at + a.max_moves;
   uint16_t* k = a.k + b * a.batch_stride;
   uint16_t* v = a.v + b * a.batch_stride;
-  for (int i = blockIdx.x; i < count; i += gridDim.x) {
+  // narrow rows several at a time
+  const int at_once = rows_at_once(a.row_chunks), sub = at_once > 1 ? threadIdx.x / a.row_chunks : 0;
+  const int first_ch = threadIdx.x - sub * a.row_chunks;
+  for (int i = blockIdx.x * at_once + sub; i < count && sub < at_once; i += gridDim.x * at_once) {
     const int to = hole_at[i], from = mover_at[i];
     const long long k_to = to * a.row_stride, k_from = from * a.row_stride;
-    for (int ch = threadIdx.x; ch < a.row_chunks; ch += 512) {
+    for (int ch = first_ch; ch < a.row_chunks; ch += 512) {
       const bool more = ch + 256 < a.row_chunks;
       uint4 x2 = make_uint4(0u, 0u, 0u, 0u), y2 = x2;
       const uint4 x = load_once((const uint4*)(k + k_from) + ch), y = load_once((const uint4*)(v + k_from) + ch);
@@ -510,8 +584,9 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
         ((uint4*)(v + k_to))[ch + 256] = y2;
       }
     }
-    if (threadIdx.x == 0) move_tables(a, b, to, from);
+    if (first_ch == 0) move_tables(a, b, to, from);
   }
+  if (LONG && blockIdx.x == 0 && threadIdx.x == 0) a.lengths_out[b] = long_state(a, b).found[2];
   if (!LONG || (a.weight_out == a.weight && a.pos_out == a.pos && a.kept == nullptr)) return;
   const LongState s = long_state(a, b);
   const size_t at = (size_t)b * a.capacity;
@@ -523,8 +598,8 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
     }
 }
 
-// The largest capacity that one workgroup selects from (its registers end here): so far its launch is the quicker form
-// (16000 slots, one request 26 us, the launches of the long form 39; eight requests 42 / 59).
+// The largest capacity that one workgroup selects from (its registers end here): so far its launch is the quicker form, or as
+// quick (one request of 16000 27.9 us, the launches of the long form 28.3; of 9000 21.6 / 26.5; eight of 16000 47.4 / 49.3).
 constexpr int SELECT_CAPACITY = 16384;
 
 static size_t move_bytes(int batch, int capacity, int budget) {
@@ -533,7 +608,7 @@ static size_t move_bytes(int batch, int capacity, int budget) {
 }
 
 size_t evict_workspace_bytes(int batch, int capacity, int budget) {
-  return move_bytes(batch, capacity, budget) + (capacity > SELECT_CAPACITY ? (size_t)batch * long_state_bytes(capacity) : 0);
+  return move_bytes(batch, capacity, budget) + (capacity > SELECT_CAPACITY ? (size_t)batch * long_state_bytes(capacity, budget) : 0);
 }
 
 hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st) {
@@ -542,13 +617,13 @@ hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st) {
   a.moves = (int32_t*)workspace;
   if (a.capacity > SELECT_CAPACITY) {
     a.long_state = (char*)workspace + move_bytes(a.batch, a.capacity, a.budget);
-    const dim3 grid((a.capacity + SEG - 1) / SEG, a.batch);
+    const dim3 grid(long_segs(a.capacity, a.budget), a.batch);
     hipLaunchKernelGGL(evict_long_top_kernel, grid, dim3(SEG_THREADS), 0, st, a);
     hipLaunchKernelGGL(evict_long_pass_kernel<0>, grid, dim3(SEG_THREADS), 0, st, a);
     hipLaunchKernelGGL(evict_long_pass_kernel<1>, grid, dim3(SEG_THREADS), 0, st, a);
     hipLaunchKernelGGL(evict_long_pass_kernel<2>, grid, dim3(SEG_THREADS), 0, st, a);
     hipLaunchKernelGGL(evict_long_pass_kernel<PASSES>, grid, dim3(SEG_THREADS), 0, st, a);
-    hipLaunchKernelGGL(evict_long_moves_kernel, dim3(a.batch), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(evict_long_moves_kernel, grid, dim3(256), 0, st, a);
   } else {
     // up to 128 KB of K and V to move for a request: by its selecting workgroup, a launch less (32 caches, 32 rows of 4 KB each:
     // 13.4 us, with the launch 14.6; 64 rows 19.1 / 17.7; 8 caches, 16 rows of 16 KB 14.5 / 13.4; 32 caches, 128 rows of 1 KB 14.3 /
@@ -563,7 +638,8 @@ hipError_t launch_cache_evict(EvictArgs a, void* workspace, hipStream_t st) {
   if (e != hipSuccess || (one_workgroup && (a.max_moves == 0 || a.fused))) return e;
   int groups = 8192 / a.batch;
   if (groups < 16) groups = 16;
-  const int useful = one_workgroup ? a.max_moves : a.max_moves + (a.capacity + 255) / 256;
+  const int at_once = rows_at_once(a.row_chunks), iterations = (a.max_moves + at_once - 1) / at_once;
+  const int useful = one_workgroup ? iterations : iterations + (a.capacity + 255) / 256;
   if (groups > useful) groups = useful;
   if (one_workgroup) hipLaunchKernelGGL(evict_move_kernel<false>, dim3(groups, a.batch), dim3(256), 0, st, a);
   else hipLaunchKernelGGL(evict_move_kernel<true>, dim3(groups, a.batch), dim3(256), 0, st, a);

@@ -551,6 +551,16 @@ def test_eviction_from_caches_that_several_workgroups_select_from(values):
     Cache(lengths, 16500, seed=13, values=values).run_and_check(16384, 0, 5000)
 
 
+@pytest.mark.parametrize("values", ["equal", "odd", "spread"])
+@pytest.mark.parametrize("capacity,budget", [(16385, 2048), (16385, 2049), (20000, 63), (20480, 18432), (30001, 29990), (40000, 50000)])
+def test_eviction_from_segments_cut_at_the_budget(values, capacity, budget):
+    """More slots than one workgroup selects from: whole and broken segments on either side of the budget; idle and short requests."""
+    lengths = [capacity, -1, budget + 1, budget, capacity - 2047, 0, capacity + 5]
+    lengths = [min(n, capacity) for n in lengths[:6]] + lengths[6:]
+    c = Cache(lengths, capacity, heads=(3, 64), seed=capacity + budget, values=values)
+    c.run_and_check(budget, min(4, budget // 3), budget // 3, in_place=values == "odd")
+
+
 def test_eviction_over_many_words():
     """More 64-slot words than a workgroup has threads."""
     Cache([200000], 200000, heads=(1, 64), seed=6, values="spread").run_and_check(150000, 4, 1000)
