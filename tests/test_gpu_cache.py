@@ -183,6 +183,17 @@ def test_lengths_far_below_their_bound(batch, q_len):
             Step((4, 2, 64), lengths, q_len, seed=31, max_len=max_len, slack=0).run_and_check()
 
 
+@pytest.mark.parametrize("heads,batch,q_len,prefix", [((32, 8, 128), 33, 4, 5000), ((32, 8, 128), 70, 9, 1000), ((8, 2, 64), 300, 1, 17000)])
+def test_long_caches_behind_a_prefix_of_much_work(heads, batch, q_len, prefix):
+    """The prefix by shared tiles and the caches in several ranges, by the lengths and, above 256 requests, by their bound."""
+    rng = np.random.default_rng(batch)
+    lengths = [int(x) for x in np.exp(rng.uniform(0, 6, batch))]
+    lengths[1], lengths[7], lengths[batch - 2] = 1250, -1, 0
+    s = Step(heads, lengths, q_len, prefix=prefix, seed=33, max_len=1300)
+    assert s.shared_tiles()
+    s.run_and_check()
+
+
 def test_without_weights_and_alone():
     """One request that one workgroup per head serves, and the same as part of a batch, without the weights."""
     for lengths in ([90], [90, 400, -1]):
