@@ -565,8 +565,8 @@ typedef struct lazyllm_kv_cache {
  * New token t of a request sees the prefix, the request's cached tokens and its new tokens up to t.  Keys and
  * values that some new token of a request sees must be finite; what lies elsewhere is of no account.
  * Sums and softmax statistics are fp32 and o is rounded once; a probability enters the product with V as two bf16
- * terms (value and remainder), against a prefix of many query rows as one.  The same call gives the same bits every
- * time; other requests' lengths, another bound on them, another batch or a prefix can change the order of a row's sums. */
+ * terms (value and remainder).  The same call gives the same bits every time; other requests' lengths, another bound on
+ * them, another batch or a prefix can change the order of a row's sums. */
 typedef struct lazyllm_step_attention {
   const void *q, *k_new, *v_new;
   void* o;

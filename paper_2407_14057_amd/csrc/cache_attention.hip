@@ -560,12 +560,13 @@ __global__ void __launch_bounds__(64 * MW) cache_merge_kernel(CacheAttentionArgs
 // all of a tile.  Products and layout as above, but V's operand comes out of LDS through the transposing read
 // (ds_read_b64_tr_b16: of four keys' 16 dimensions, lane c gets dimension c of the four), so no vector instruction is
 // spent on it.  The sum of the exponentials is one more row tile of the second product (V = 1): it costs the
-// matrix pipe 1/16 and spares the vector unit, the busier one, an addition per probability.  P is rounded to bf16 once
-// here (the remainder term would cost a third of all MFMAs); the sum is taken over the rounded values.
-// What bounds it: a step takes 4.0 k cycles of a SIMD, 2.2 k of them the matrix pipe, 2 k vector instructions, while the CU's LDS
-// moves 288 KB; without the LDS reads it would take 3.0 k, without the copies 3.4 k.  Kept in opposite phases by two
-// barriers a step, or with the next scores under the exponentials, the two waves of a SIMD were no faster (300, 280 us
-// where this takes 268: 2048 rows of 8 K,V heads, 32768 keys); nor were three row tiles a wave (314).
+// matrix pipe 1/13 and spares the vector unit an addition per probability.  P goes into the second product as two bf16
+// terms, as above, so that a request's accuracy does not depend on how many others are in its batch: 2048 rows of 8 K,V
+// heads behind 32768 keys 353 us and 1.66e-3 off (the rounding of the output), with one term 264 us and 2.33e-3.
+// What bounds it there: of the 5.5 k cycles that a step takes a SIMD, 3.3 k are the matrix pipe's; 420 vector instructions,
+// 128 of them exponentials, go on beside it.  With one term, the two waves of a SIMD kept in opposite phases by two
+// barriers a step, or with the next scores under the exponentials, were no faster (300, 280 us where this took 268); nor
+// were three row tiles a wave (314).
 template <int HD>
 __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttentionArgs a) {
   constexpr int KS = HD / 32, NT = HD / 16, BN = 64, T = 2, NW = 8;
@@ -705,7 +706,7 @@ __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttention
           if (k0 + 16 * sub + 4 * g + r >= a.prefix_len)
 #pragma unroll
             for (int t = 0; t < T; ++t) s[t][sub][r] = -INFINITY;
-    uint4 p[T][2];
+    uint4 p_hi[T][2], p_lo[T][2];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       float top = s[t][0][0];
@@ -732,14 +733,20 @@ __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttention
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           e[j] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * u + (j >> 2)][j & 3], a.scale_log2e, neg_m));
-        p[t][u] = pack8(e);
+        float rest[8];
+        p_hi[t][u] = pack8(e);
+        unpack8(p_hi[t][u], rest);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) rest[j] = e[j] - rest[j];
+        p_lo[t][u] = pack8(rest);
       }
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
 #pragma unroll
-      for (int t = 0; t < T; ++t)
-        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, *(const bf16x8_t*)&p[t][u], sum[t], 0, 0, 0);
+      for (int t = 0; t < T; ++t) sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, *(const bf16x8_t*)&p_hi[t][u], sum[t], 0, 0, 0);
+#pragma unroll
+      for (int t = 0; t < T; ++t) sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, *(const bf16x8_t*)&p_lo[t][u], sum[t], 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
         short4_t half[2];
@@ -749,16 +756,19 @@ __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttention
         const short8_t both = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
         for (int t = 0; t < T; ++t)
-          acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8_t*)&both, *(const bf16x8_t*)&p[t][u], acc[t][i], 0, 0, 0);
+          acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8_t*)&both, *(const bf16x8_t*)&p_hi[t][u], acc[t][i], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+          acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8_t*)&both, *(const bf16x8_t*)&p_lo[t][u], acc[t][i], 0, 0, 0);
       }
     }
     __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
 #pragma unroll
     for (int u = 0; u < 2 * NT - 6; ++u) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(0x008, 16, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 32, 0);
     __builtin_amdgcn_sched_barrier(0);
   }
   const size_t all_rows = (size_t)a.batch * a.q_len * a.n_heads;

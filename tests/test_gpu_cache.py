@@ -282,6 +282,25 @@ def test_shared_prefix_of_few_keys_and_very_many_rows():
     s.run_and_check()
 
 
+@pytest.mark.parametrize("heads,batch,q_len,prefix", [("32/8x128", 128, 8, 613), ("4/2x64", 300, 64, 520)])
+def test_accuracy_behind_a_prefix_does_not_depend_on_the_number_of_query_rows(heads, batch, q_len, prefix):
+    """Shared tiles are as accurate as the direct form that fewer rows take: check() with the direct form's bound, in which a
+    probability is off by 2^-16 of itself (two bf16 terms: 2^-8 of the remainder, which is 2^-8 of the value at most).
+    Every second key of the prefix has the weight 1 and a value near -1, the others r = exp(-q_0 / sqrt(hd)) and 1, so that
+    o is near (r - 1) / (r + 1), a few hundredths, and r rounded once, off by up to 2^-9, moves it by 2^-9 * 2 / (r + 1)^2 =
+    1e-3, where the bound is 2^-8 |o| + 1e-4 = 3e-4."""
+    rng = np.random.default_rng(prefix)
+    s = Step(HEADS[heads], [int(x) for x in rng.integers(-1, 9, batch)], q_len, prefix=prefix, seed=prefix)
+    assert s.shared_tiles()
+    s.q[..., 1:] = 0
+    s.q[..., 0] = s.q[..., 0].abs().clamp(0.5, 2.0)
+    s.pk.zero_()
+    s.pk[1::2, :, 0] = -1
+    s.pv[::2], s.pv[1::2] = -1, 1
+    s.shared_tiles = lambda: False
+    s.run_and_check()
+
+
 @pytest.mark.parametrize("prefix", [0, 200])
 def test_strided_caches(prefix):
     """K and V rows interleaved in one buffer, as [slot][2][heads][dim]."""
