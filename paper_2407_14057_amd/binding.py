@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -92,6 +93,8 @@ class lazyllm_step_attention(C.Structure):
                 ("prefix_stride", C.c_int64), ("weight", C.c_void_p), ("weight_out", C.c_void_p),
                 ("pos_new", C.c_void_p), ("pos", C.c_void_p), ("status", C.c_void_p)]
 
+
+_STEP_LAYOUT = struct.Struct("@5P4i2Pq5P")        # of lazyllm_step_attention
 
 STEP_NAMES = ("plan", "rope_table", "embed", "select", "gather", "rmsnorm", "gemm_qkv", "v_transpose",
               "score", "attention", "gemm_o", "gemm_gate_up", "gemm_down", "lm_head")
@@ -480,6 +483,43 @@ def _cache_stream(cache: lazyllm_kv_cache, workspace: torch.Tensor, stream: Opti
     return torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream
 
 
+def _operand(t, here: int, dtype: torch.dtype, count: int) -> int:
+    """Address of an operand: `count` values of a type, one behind the other, on the device `here`.  Anything else is refused (the
+    library gets addresses alone); an address in place of a tensor is taken as it is."""
+    try:
+        if t.get_device() == here and t.dtype is dtype and t.numel() == count and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:                    # (no tensor)
+        if type(t) is int:
+            return t
+    raise LazyLLMError(LAZYLLM_EINVAL)
+
+
+def _status(t, here: int) -> Optional[int]:
+    return None if t is None else _operand(t, here, torch.int32, 1 if type(t) is int else max(1, t.numel()))
+
+
+def _room(workspace: torch.Tensor) -> Tuple[int, int]:
+    if not workspace.is_contiguous():
+        raise LazyLLMError(LAZYLLM_EINVAL)
+    return workspace.data_ptr(), workspace.nbytes
+
+
+def _step(cache, q, k_new, v_new, lengths, n_heads, q_len, max_len, o, here, prefix_len, prefix_k, prefix_v, prefix_stride, weight,
+          weight_out, pos_new, pos, status) -> lazyllm_step_attention:
+    batch, slots = cache.batch, cache.batch * cache.capacity
+    rows, new, bf16, i32, f32 = (batch * q_len * n_heads * cache.head_dim, batch * q_len * cache.n_kv_heads * cache.head_dim, torch.bfloat16,
+                                 torch.int32, torch.float32)
+    # (packed at once: the constructor takes twice as long for its 17 members; 0 is NULL)
+    return lazyllm_step_attention.from_buffer_copy(_STEP_LAYOUT.pack(
+        _operand(q, here, bf16, rows), _operand(k_new, here, bf16, new), _operand(v_new, here, bf16, new), _operand(o, here, bf16, rows),
+        _operand(lengths, here, i32, batch), n_heads, q_len, max_len, prefix_len, prefix_k, prefix_v, prefix_stride,
+        0 if weight is None else _operand(weight, here, f32, slots),
+        0 if weight_out is None else _operand(weight_out, here, f32, slots),
+        0 if pos_new is None else _operand(pos_new, here, i32, batch),
+        0 if pos is None else _operand(pos, here, i32, slots), _status(status, here) or 0))
+
+
 def lazyllm_op_cache_attention_workspace_bytes(cache: lazyllm_kv_cache, n_heads: int, q_len: int, max_len: int,
                                                prefix_len: int = 0, weights: bool = False) -> int:
     return int(lib().lazyllm_op_cache_attention_workspace_bytes(C.byref(cache), n_heads, q_len, max_len, prefix_len,
@@ -488,26 +528,29 @@ def lazyllm_op_cache_attention_workspace_bytes(cache: lazyllm_kv_cache, n_heads:
 
 def lazyllm_op_cache_attention(cache, q, k_new, v_new, lengths, n_heads, q_len, max_len, o, workspace, weight=None,
                                weight_out=None, pos_new=None, pos=None, status=None, stream=None) -> None:
-    s = lazyllm_step_attention(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(o), _ptr(lengths), n_heads, q_len, max_len, 0, None,
-                               None, 0, _ptr(weight), _ptr(weight_out), _ptr(pos_new), _ptr(pos), _ptr(status))
-    _check(lib().lazyllm_op_cache_attention(C.byref(cache), C.byref(s), _ptr(workspace),
-                                            workspace.nbytes, _cache_stream(cache, workspace, stream)))
+    """Tensors as the header documents them: contiguous, of those types and sizes, on the current device."""
+    on = _cache_stream(cache, workspace, stream)
+    s = _step(cache, q, k_new, v_new, lengths, n_heads, q_len, max_len, o, workspace.get_device(), 0, 0, 0, 0, weight, weight_out, pos_new,
+              pos, status)
+    _check(lib().lazyllm_op_cache_attention(C.byref(cache), C.byref(s), *_room(workspace), on))
 
 
 def lazyllm_op_prefix_attention(cache, prefix_k, prefix_v, q, k_new, v_new, lengths, n_heads, q_len, max_len, o, workspace,
                                 weight=None, weight_out=None, pos_new=None, pos=None, status=None, stream=None) -> None:
-    """prefix_k, prefix_v: [prefix_len, n_kv_heads, head_dim], possibly strided from row to row."""
+    """prefix_k, prefix_v: [prefix_len, n_kv_heads, head_dim], possibly strided from row to row; the rest as in
+    lazyllm_op_cache_attention."""
     shape, stride = prefix_k.shape, prefix_k.stride()
     if (prefix_k.dtype != torch.bfloat16 or prefix_v.dtype != torch.bfloat16 or shape != prefix_v.shape or
             stride != prefix_v.stride() or len(shape) != 3 or shape[0] < 1 or shape[1] != cache.n_kv_heads or
             shape[2] != cache.head_dim or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2])):
         raise LazyLLMError(LAZYLLM_EINVAL)
+    on, here = _cache_stream(cache, workspace, stream), workspace.get_device()
+    if prefix_k.get_device() != here or prefix_v.get_device() != here:
+        raise LazyLLMError(LAZYLLM_EINVAL)
     row = stride[0] if shape[0] > 1 else shape[1] * shape[2]
-    s = lazyllm_step_attention(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(o), _ptr(lengths), n_heads, q_len, max_len,
-                               shape[0], prefix_k.data_ptr(), prefix_v.data_ptr(), row, _ptr(weight),
-                               _ptr(weight_out), _ptr(pos_new), _ptr(pos), _ptr(status))
-    _check(lib().lazyllm_op_prefix_attention(C.byref(cache), C.byref(s), _ptr(workspace),
-                                             workspace.nbytes, _cache_stream(cache, workspace, stream)))
+    s = _step(cache, q, k_new, v_new, lengths, n_heads, q_len, max_len, o, here, shape[0], prefix_k.data_ptr(), prefix_v.data_ptr(), row, weight,
+              weight_out, pos_new, pos, status)
+    _check(lib().lazyllm_op_prefix_attention(C.byref(cache), C.byref(s), *_room(workspace), on))
 
 
 def lazyllm_op_cache_evict_workspace_bytes(cache: lazyllm_kv_cache, budget: int) -> int:
@@ -516,9 +559,13 @@ def lazyllm_op_cache_evict_workspace_bytes(cache: lazyllm_kv_cache, budget: int)
 
 def lazyllm_op_cache_evict(cache, weight, pos, lengths, budget, sinks, recent, weight_out, pos_out, lengths_out, workspace,
                            kept=None, status=None, stream=None) -> None:
-    _check(lib().lazyllm_op_cache_evict(C.byref(cache), _ptr(weight), _ptr(pos), _ptr(lengths), budget, sinks, recent,
-                                        _ptr(weight_out), _ptr(pos_out), _ptr(lengths_out), _ptr(kept), _ptr(status),
-                                        _ptr(workspace), workspace.nbytes, _cache_stream(cache, workspace, stream)))
+    """Tensors as the header documents them: contiguous, of those types and sizes, on the current device."""
+    on = _cache_stream(cache, workspace, stream)
+    here, batch, slots, i32, f32 = workspace.get_device(), cache.batch, cache.batch * cache.capacity, torch.int32, torch.float32
+    _check(lib().lazyllm_op_cache_evict(
+        C.byref(cache), _operand(weight, here, f32, slots), _operand(pos, here, i32, slots), _operand(lengths, here, i32, batch), budget, sinks,
+        recent, _operand(weight_out, here, f32, slots), _operand(pos_out, here, i32, slots), _operand(lengths_out, here, i32, batch),
+        None if kept is None else _operand(kept, here, i32, batch * budget), _status(status, here), *_room(workspace), on))
 
 
 # ---------------------------------------------------------------------------- decoding steps

@@ -173,3 +173,96 @@ def test_what_is_not_on_the_current_device_is_refused(monkeypatch):
         with pytest.raises(B.LazyLLMError) as e:
             call()
         assert e.value.status == B.LAZYLLM_EINVAL
+
+
+class _Library:
+    """Stands for the library: counts the calls that reach it."""
+
+    def __init__(self, real):
+        self.real, self.reached = real, 0
+
+    def __getattr__(self, name):
+        return self._reach if name.startswith("lazyllm_op_") else getattr(self.real, name)
+
+    def _reach(self, *args):
+        self.reached += 1
+        return B.LAZYLLM_OK
+
+
+class _Elsewhere(torch.Tensor):
+    def get_device(self):
+        return 3
+
+
+def _operands(n_heads=4, q_len=2, batch=3, capacity=20, kvh=2, hd=64, budget=5, prefix=7):
+    bf, i32 = torch.bfloat16, torch.int32
+    k = torch.zeros(batch, capacity, kvh, hd, dtype=bf)
+    t = dict(q=torch.zeros(batch, q_len, n_heads, hd, dtype=bf), k_new=torch.zeros(batch, q_len, kvh, hd, dtype=bf),
+             v_new=torch.zeros(batch, q_len, kvh, hd, dtype=bf), o=torch.zeros(batch, q_len, n_heads, hd, dtype=bf),
+             lengths=torch.zeros(batch, dtype=i32), weight=torch.zeros(batch, capacity), weight_out=torch.zeros(batch, capacity),
+             pos_new=torch.zeros(batch, dtype=i32), pos=torch.zeros(batch, capacity, dtype=i32), status=torch.zeros(1, dtype=i32),
+             pos_out=torch.zeros(batch, capacity, dtype=i32), lengths_out=torch.zeros(batch, dtype=i32),
+             kept=torch.zeros(batch, budget, dtype=i32), prefix_k=torch.zeros(prefix, kvh, hd, dtype=bf),
+             prefix_v=torch.zeros(prefix, kvh, hd, dtype=bf))
+    return B.make_kv_cache(k, k.clone()), t
+
+
+def _call(name, cache, t, ws, stream):
+    if name == "evict":
+        B.lazyllm_op_cache_evict(cache, t["weight"], t["pos"], t["lengths"], 5, 1, 1, t["weight_out"], t["pos_out"], t["lengths_out"], ws,
+                                 kept=t["kept"], status=t["status"], stream=stream)
+        return
+    args = (t["q"], t["k_new"], t["v_new"], t["lengths"], 4, 2, 18, t["o"], ws)
+    more = {k: t[k] for k in ("weight", "weight_out", "pos_new", "pos", "status")}
+    if name == "prefix":
+        B.lazyllm_op_prefix_attention(cache, t["prefix_k"], t["prefix_v"], *args, **more, stream=stream)
+    else:
+        B.lazyllm_op_cache_attention(cache, *args, **more, stream=stream)
+
+
+OPERANDS = {"attention": ["q", "k_new", "v_new", "o", "lengths", "weight", "weight_out", "pos_new", "pos", "status"],
+            "evict": ["weight", "pos", "lengths", "weight_out", "pos_out", "lengths_out", "kept", "status"]}
+OPERANDS["prefix"] = OPERANDS["attention"] + ["prefix_k", "prefix_v"]
+
+
+@pytest.mark.parametrize("name", list(OPERANDS))
+def test_operands_of_another_device_type_size_or_layout_are_refused(name, monkeypatch):
+    """Every tensor of a call, one at a time; the library, which gets addresses alone, is not reached."""
+    library = _Library(B.lib())
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)              # (where the tensors here are)
+    monkeypatch.setattr(B, "_lib_handle", library)
+
+    class Stream:
+        device_index, cuda_stream = -1, 77
+
+    ws = torch.zeros(4096, dtype=torch.uint8)
+    cache, good = _operands()
+    _call(name, cache, good, ws, Stream)
+    assert library.reached == 1
+    # stacked tables, and a status that is one of several, are as good; what may be left out may be left out
+    for change in ([{"status": torch.zeros(4, dtype=torch.int32)}, {"status": None}, {"lengths": good["lengths"].view(1, 3)}] +
+                   ([{"kept": None}] if name == "evict" else [{"weight": None, "weight_out": None}, {"pos": None, "pos_new": None}])):
+        _call(name, cache, dict(good, **change), ws, Stream)
+    reached = library.reached
+    for operand in OPERANDS[name]:
+        t = good[operand]
+        bad = [t.as_subclass(_Elsewhere), t.to(torch.float64), t.to(torch.int64), t[:0]]
+        if operand != "status":
+            wide = torch.zeros(*t.shape[:-1], 2 * t.shape[-1], dtype=t.dtype)
+            bad += [t[:-1], torch.cat([t, t]), wide, wide[..., ::2]]            # (the last: the right size, with gaps)
+        for wrong in bad:
+            with pytest.raises(B.LazyLLMError) as e:
+                _call(name, cache, dict(good, **{operand: wrong}), ws, Stream)
+            assert e.value.status == B.LAZYLLM_EINVAL, (operand, wrong.shape, wrong.dtype)
+    for operand in ("q", "k_new", "v_new", "o", "lengths") if name != "evict" else OPERANDS[name][:6]:
+        with pytest.raises(B.LazyLLMError) as e:                                # what has to be there
+            _call(name, cache, dict(good, **{operand: None}), ws, Stream)
+        assert e.value.status == B.LAZYLLM_EINVAL
+    assert library.reached == reached
+
+
+def test_layout_of_a_step():
+    """The binding packs a step's members at once: in the order and with the sizes of the structure."""
+    assert B._STEP_LAYOUT.size == C.sizeof(B.lazyllm_step_attention)
+    s = B.lazyllm_step_attention.from_buffer_copy(B._STEP_LAYOUT.pack(*range(1, 18)))
+    assert [getattr(s, name) for name, _ in s._fields_] == list(range(1, 18))
