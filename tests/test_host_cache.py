@@ -1,5 +1,6 @@
 """The entry points over a batch's K,V caches refuse bad arguments on the host, before any HIP call (no GPU here)."""
 import ctypes as C
+import os
 
 import pytest
 import torch
@@ -266,3 +267,24 @@ def test_layout_of_a_step():
     assert B._STEP_LAYOUT.size == C.sizeof(B.lazyllm_step_attention)
     s = B.lazyllm_step_attention.from_buffer_copy(B._STEP_LAYOUT.pack(*range(1, 18)))
     assert [getattr(s, name) for name, _ in s._fields_] == list(range(1, 18))
+
+
+def test_step_of_the_readme_leaves_idle_requests_idle(monkeypatch):
+    """The README's step, run on the host with calls that do nothing: a request whose length is negative takes no part in the
+    next step either, the others have one token more."""
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        step = [block for block in f.read().split("```")[1::2] if "B.make_kv_cache(" in block]
+    assert len(step) == 1
+    calls = []
+
+    class Calls:
+        def __getattr__(self, name):
+            calls.append(name)
+            return lambda *args, **kwargs: 1
+
+    lengths = torch.tensor([3, -1, 0, -7], dtype=torch.int32)
+    monkeypatch.setattr(torch, "empty", lambda *args, **kwargs: None)
+    names = ("k v n_heads max_len q k_new v_new o weight pos budget sinks recent evict_ws").split()
+    exec(step[0], dict(dict.fromkeys(names), B=Calls(), torch=torch, lengths=lengths, position=lengths.clone()))
+    assert "lazyllm_op_cache_attention" in calls and "lazyllm_op_cache_evict" in calls
+    assert lengths.tolist() == [4, -1, 1, -7] and lengths.dtype == torch.int32
