@@ -591,9 +591,14 @@ size_t lazyllm_op_cache_attention_workspace_bytes(const lazyllm_kv_cache* cache,
 /* Attention of the new tokens over the requests' own caches; the prefix members of *step are ignored. */
 int lazyllm_op_cache_attention(const lazyllm_kv_cache* cache, const lazyllm_step_attention* step, void* workspace,
                                size_t ws_bytes, void* hip_stream);
-/* The same behind a common prefix of prefix_len >= 1 tokens, which is read once for all requests. */
+/* The same behind a common prefix of prefix_len >= 1 tokens, which is read once for every
+ * lazyllm_op_prefix_attention_block query rows of a K,V head, of whichever requests they are. */
 int lazyllm_op_prefix_attention(const lazyllm_kv_cache* cache, const lazyllm_step_attention* step, void* workspace,
                                 size_t ws_bytes, void* hip_stream);
+
+/* How many query rows of a K,V head (batch * q_len * n_heads / n_kv_heads in all) go over the prefix together: 16, 32 or,
+ * where that pays, 256, through tiles that eight waves share.  Host only.  LAZYLLM_EINVAL on a bad argument. */
+int lazyllm_op_prefix_attention_block(const lazyllm_kv_cache* cache, int32_t n_heads, int32_t q_len, int32_t prefix_len);
 
 /* Eviction: a request with more than `budget` tokens keeps `budget` of them (the rule of Sec. 3.2 on accumulated
  * weights): first those whose position is below `sinks` or among the last `recent` positions (above the request's

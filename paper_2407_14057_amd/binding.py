@@ -189,6 +189,7 @@ _SIGNATURES = {
                                              C.c_void_p, C.c_size_t, C.c_void_p]),
     "lazyllm_op_prefix_attention": (C.c_int, [C.POINTER(lazyllm_kv_cache), C.POINTER(lazyllm_step_attention),
                                               C.c_void_p, C.c_size_t, C.c_void_p]),
+    "lazyllm_op_prefix_attention_block": (C.c_int, [C.POINTER(lazyllm_kv_cache), C.c_int32, C.c_int32, C.c_int32]),
     "lazyllm_op_cache_evict_workspace_bytes": (C.c_size_t, [C.POINTER(lazyllm_kv_cache), C.c_int32]),
     "lazyllm_op_cache_evict": (C.c_int, [C.POINTER(lazyllm_kv_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
                                          C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,

@@ -1414,6 +1414,12 @@ int lazyllm_op_prefix_attention(const lazyllm_kv_cache* cache, const lazyllm_ste
   return step_attention(cache, *step, workspace, ws_bytes, (hipStream_t)hip_stream);
 }
 
+int lazyllm_op_prefix_attention_block(const lazyllm_kv_cache* c, int32_t n_heads, int32_t q_len, int32_t prefix_len) {
+  if (!kv_cache_shape_ok(c) || !step_shape_ok(c, n_heads, q_len, 0) || prefix_len < 1 || prefix_len > (1 << 30)) return LAZYLLM_EINVAL;
+  const CacheAttentionPlan plan = cache_attention_plan(c->batch, n_heads, c->n_kv_heads, c->head_dim, q_len, 0, prefix_len, false);
+  return plan.shared_tiles ? 256 : 16 * plan.tiles;
+}
+
 size_t lazyllm_op_cache_evict_workspace_bytes(const lazyllm_kv_cache* c, int32_t budget) {
   if (!kv_cache_shape_ok(c) || budget < 1 || c->capacity > EVICT_MAX_CAPACITY) return 0;
   return evict_workspace_bytes(c->batch, c->capacity, budget);

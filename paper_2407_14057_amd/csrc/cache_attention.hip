@@ -7,7 +7,7 @@
 //
 // One pass over K and V with a running maximum and sum.  A work item is a K,V head, a block of its query rows and a
 // range of keys; the query rows of a K,V head are the (token, query head of the group) pairs of one request for a
-// range of its own cache, and those of ALL requests for a range of the prefix, which is therefore read once.
+// range of its own cache, and those of ALL requests for a range of the prefix, which is therefore read once for a block of rows.
 // The partial results (output, maximum, sum) of the ranges are merged by a second launch.
 #include <algorithm>
 #include <type_traits>
@@ -783,11 +783,12 @@ __global__ void __launch_bounds__(512, 2) prefix_attention_kernel(CacheAttention
 }
 
 // How a call is cut, measured (us):
-//  - the prefix through shared tiles where its work, query rows of a K,V head x keys x K,V heads x head_dim, is above
-//    2.5 G and there are 128 rows or more: below that the launch more costs more than the tiles save.  In units of 128 M
-//    (rows x keys, 8 K,V heads of 128), direct / shared: 256 x 4000 = 8.2: 23 / 30; 128 x 16000 = 16: 32 / 35; 512 x 4000 =
-//    16: 32 / 34; 128 x 32000 = 33: 62 / 54; 256 x 16000 = 33: 52 / 44; 1024 x 4000 = 33: 53 / 40; 2048 x 32000 = 524:
-//    597 / 254; 32 heads, 64 x 16000 = 33: 77 / 90; 4 heads of 64, 512 x 4000 = 4: 17 / 22, 256 x 32000 = 16: 43 / 30.
+//  - the prefix through shared tiles (blocks of 256 query rows) from 42 M logits on: keys x K,V heads x query rows, less the
+//    rows that are missing in the last block, which cost as much.  Below, the launch more costs more than the tiles save.
+//    Direct / shared, at 36, 44 and 66 M: 256 rows of 8 K,V heads of 128: 50 / 50, 59 / 55, 87 / 70; 512: 45 / 46, 51 / 51, 72 / 65;
+//    2048: 56 / 57, 61 / 62, 76 / 72; 256 of 32 heads: 63 / 66, 71 / 71, 94 / 86; 2048 of one: 44 / 47, 51 / 52, 72 / 65; 256 of 4
+//    heads of 64: 36 / 40, 41 / 43, 58 / 50; 1024: 35 / 36, 41 / 39, 56 / 47; 2048 of 8 heads of 64: 35 / 41, 39 / 45, 50 / 52.  Blocks in part
+//    empty, at 44 and 66 M without that: 128 rows of 8 heads: 71 / 78, 98 / 107; 192: 67 / 63, 96 / 82; 288: 66 / 72, 97 / 96.
 //  - row tiles: one up to 16 rows, else two (a prefix of 3376 for 128 rows: 20.1 with one, 16.6 with two).
 //  - ranges of the caches, up to 256 requests: by the lengths, which the host does not know; every workgroup finds its range
 //    from all of them.  About 256 ranges x K,V heads a request, at most 2048 (one row tile) or 512 (two: as many workgroups
@@ -813,7 +814,8 @@ CacheAttentionPlan cache_attention_plan(int batch, int n_heads, int n_kv, int he
   CacheAttentionPlan p{};
   const int group = n_heads / n_kv;
   const long long own_rows = (long long)q_len * group, prefix_rows = prefix_len > 0 ? own_rows * batch : 0;
-  p.shared_tiles = prefix_rows >= 128 && (double)prefix_rows * prefix_len * n_kv * head_dim >= 2.5e9;
+  const long long missing = (prefix_rows + 255) / 256 * 256 - prefix_rows;
+  p.shared_tiles = (double)(prefix_rows - missing) * prefix_len * n_kv >= 42e6;
   p.tiles = (p.shared_tiles || prefix_rows < own_rows ? own_rows : prefix_rows) <= 16 ? 1 : 2;
   const int rows = 16 * p.tiles, shared_rows = p.shared_tiles ? 256 : rows;
   p.own_blocks = (int)((own_rows + rows - 1) / rows);

@@ -1,5 +1,6 @@
 """A batch's K,V caches on the GPU: attention of the new tokens (with and without a shared prefix), Eq. 1's weights kept up to
 date, eviction.  Against plain implementations in 64 bits; everything that must not be read holds NaN."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -282,7 +283,14 @@ def test_shared_prefix_of_few_keys_and_very_many_rows():
     s.run_and_check()
 
 
-@pytest.mark.parametrize("heads,batch,q_len,prefix", [("32/8x128", 128, 8, 613), ("4/2x64", 300, 64, 520)])
+def _tiled(s):
+    """A step whose prefix goes through the tiles that 256 query rows share; they are as accurate as the direct form."""
+    assert B.lib().lazyllm_op_prefix_attention_block(C.byref(s.cache), s.H, s.q_len, s.prefix) == 256
+    s.shared_tiles = lambda: False
+    return s
+
+
+@pytest.mark.parametrize("heads,batch,q_len,prefix", [("32/8x128", 128, 8, 1297), ("4/2x64", 300, 64, 563)])
 def test_accuracy_behind_a_prefix_does_not_depend_on_the_number_of_query_rows(heads, batch, q_len, prefix):
     """Shared tiles are as accurate as the direct form that fewer rows take: check() with the direct form's bound, in which a
     probability is off by 2^-16 of itself (two bf16 terms: 2^-8 of the remainder, which is 2^-8 of the value at most).
@@ -290,15 +298,73 @@ def test_accuracy_behind_a_prefix_does_not_depend_on_the_number_of_query_rows(he
     o is near (r - 1) / (r + 1), a few hundredths, and r rounded once, off by up to 2^-9, moves it by 2^-9 * 2 / (r + 1)^2 =
     1e-3, where the bound is 2^-8 |o| + 1e-4 = 3e-4."""
     rng = np.random.default_rng(prefix)
-    s = Step(HEADS[heads], [int(x) for x in rng.integers(-1, 9, batch)], q_len, prefix=prefix, seed=prefix)
-    assert s.shared_tiles()
+    s = _tiled(Step(HEADS[heads], [int(x) for x in rng.integers(-1, 9, batch)], q_len, prefix=prefix, seed=prefix))
     s.q[..., 1:] = 0
     s.q[..., 0] = s.q[..., 0].abs().clamp(0.5, 2.0)
     s.pk.zero_()
     s.pk[1::2, :, 0] = -1
     s.pv[::2], s.pv[1::2] = -1, 1
-    s.shared_tiles = lambda: False
     s.run_and_check()
+
+
+@pytest.mark.parametrize("heads,batch,q_len,prefix", [("32/8x128", 67, 4, 9601), ("32/8x128", 67, 4, 6400), ("8/1x128", 67, 4, 21500), ("4x64", 125, 2, 43071),
+                                                      ("4x64", 64, 4, 41089), ("4/2x64", 67, 4, 69120)])
+def test_prefix_through_shared_tiles(heads, batch, q_len, prefix):
+    """Neither the last block of rows nor the last tile of keys need be full; some requests are idle."""
+    rng = np.random.default_rng(prefix)
+    _tiled(Step(HEADS[heads], [int(x) for x in rng.integers(-1, 40, batch)], q_len, prefix=prefix, seed=prefix)).run_and_check(in_place=prefix == 6400)
+
+
+def test_prefix_of_few_keys_through_shared_tiles():
+    """65 keys for 34 tokens of 64 heads on one of 300 requests each: a tile and a key."""
+    _tiled(Step((64, 1, 128), [2] * 300, 34, prefix=65, seed=3, weights=False)).run_and_check()
+
+
+@pytest.mark.parametrize("heads,batch,q_len,prefix", [((32, 8, 128), 33, 4, 18501), ((32, 8, 128), 70, 9, 2200), ((8, 2, 64), 300, 1, 19001)])
+def test_long_caches_and_a_prefix_through_shared_tiles(heads, batch, q_len, prefix):
+    """The caches in several ranges, by the lengths and, above 256 requests, by their bound."""
+    rng = np.random.default_rng(batch)
+    lengths = [int(x) for x in np.exp(rng.uniform(0, 6, batch))]
+    lengths[1], lengths[7], lengths[batch - 2] = 1250, -1, 0
+    _tiled(Step(heads, lengths, q_len, prefix=prefix, seed=33, max_len=1300)).run_and_check()
+
+
+def test_strided_prefix_and_steep_logits_through_shared_tiles():
+    _tiled(_stride_prefix(Step((4, 2, 64), [10] * 128, 2, prefix=41100, seed=12))).run_and_check()
+    s = _tiled(Step((32, 8, 128), [300, 40] + [7] * 62, 2, prefix=10300, seed=15, spread=20.0))
+    s.pk[10200:] *= 2                                         # the maximum moves late
+    s.run_and_check()
+
+
+def test_prefix_through_shared_tiles_captured_and_repeated():
+    """Two graphs of one workspace, replayed in turn, give the eager call's bits, with other inputs and lengths too."""
+    s, eager = (_tiled(Step((32, 1, 128), [3, -1, 40, 0] * 35, 1, prefix=9800, seed=19, max_len=60)) for _ in range(2))
+    s.run()                                                     # (loads the kernels outside the capture)
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            s.run(stream=torch.cuda.current_stream())
+        graphs.append(graph)
+    gen = torch.Generator().manual_seed(20)
+    for i in range(4):
+        for x in ("q", "k_new", "v_new"):
+            fresh = torch.randn(getattr(s, x).shape, generator=gen).to(torch.bfloat16).to(DEV)
+            getattr(s, x).copy_(fresh)
+            getattr(eager, x).copy_(fresh)
+        for t in (s, eager):
+            t.weight_out.fill_(-5.0)
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        eager.run_and_check()
+        assert torch.equal(s.o, eager.o) and torch.equal(s.weight_out, eager.weight_out)
+        for t in (s, eager):
+            t.weight.copy_(torch.where(t.weight_out == -5.0, t.weight, t.weight_out))
+            t.len_dev += (t.len_dev >= 0).int()
+            t.pos_new += 1
+        eager.lengths = [n + 1 if n >= 0 else n for n in eager.lengths]
+        eager.pos.fill_(-7)
 
 
 @pytest.mark.parametrize("prefix", [0, 200])

@@ -288,3 +288,35 @@ def test_step_of_the_readme_leaves_idle_requests_idle(monkeypatch):
     exec(step[0], dict(dict.fromkeys(names), B=Calls(), torch=torch, lengths=lengths, position=lengths.clone()))
     assert "lazyllm_op_cache_attention" in calls and "lazyllm_op_cache_evict" in calls
     assert lengths.tolist() == [4, -1, 1, -7] and lengths.dtype == torch.int32
+
+
+def _block(heads, rows, prefix):
+    """Query rows that go over the prefix together, of `rows` (multiples of the heads of a group) of a K,V head."""
+    n_heads, kvh, hd = heads
+    group = n_heads // kvh
+    assert rows % group == 0
+    return B.lib().lazyllm_op_prefix_attention_block(C.byref(_cache(batch=rows // group, n_kv_heads=kvh, head_dim=hd, row_stride=kvh * hd)), n_heads,
+                                                     1, prefix)
+
+
+@pytest.mark.parametrize("heads,rows,prefix,direct,shared", [
+    ((32, 8, 128), 256, 16000, 42.4, 47.6), ((32, 8, 128), 1024, 4000, 44.9, 46.8), ((32, 8, 128), 128, 32000, 57.4, 64.4),
+    ((32, 8, 128), 128, 64453, 97.9, 107.1), ((32, 32, 128), 128, 20507, 130.0, 146.6), ((32, 32, 128), 64, 16000, 75.0, 117.1),
+    ((32, 8, 128), 320, 17187, 55.7, 67.0), ((8, 1, 128), 2048, 16000, 41.8, 45.9), ((4, 4, 64), 256, 16000, 21.9, 30.7),
+    ((4, 4, 64), 1024, 8789, 34.9, 35.7), ((32, 8, 128), 256, 32226, 86.5, 69.9), ((32, 8, 128), 512, 16113, 71.8, 65.2),
+    ((32, 32, 128), 256, 8056, 93.7, 85.6), ((4, 4, 64), 256, 64453, 57.5, 50.3), ((4, 4, 64), 1024, 16113, 56.2, 46.6),
+    ((64, 8, 64), 512, 10742, 40.7, 38.6), ((8, 1, 128), 2048, 26367, 62.6, 58.0), ((4, 4, 64), 192, 85937, 73.9, 61.2)])
+def test_prefix_takes_the_form_that_was_measured_faster(heads, rows, prefix, direct, shared):
+    """us of the two forms on an MI355X."""
+    assert (_block(heads, rows, prefix) == 256) == (shared < direct)
+
+
+def test_blocks_of_query_rows_behind_a_prefix():
+    assert [_block((4, 4, 64), rows, 100) for rows in (1, 16, 17, 500)] == [16, 16, 32, 32]
+    ask = B.lib().lazyllm_op_prefix_attention_block
+    for change in BAD_CACHES:
+        assert ask(C.byref(_cache(**change)), 4, 2, 100) == B.LAZYLLM_EINVAL, change
+    for n_heads, q_len, prefix in ((0, 2, 100), (3, 2, 100), (4, 0, 100), (4, 65, 100), (4, 2, 0), (4, 2, -1), (4, 2, (1 << 30) + 1)):
+        assert ask(C.byref(_cache()), n_heads, q_len, prefix) == B.LAZYLLM_EINVAL
+    assert ask(None, 4, 2, 100) == B.LAZYLLM_EINVAL
+    assert ask(C.byref(_cache()), 4, 2, 1 << 30) == 16                 # (12 rows; a block of 256 would be nearly empty)
