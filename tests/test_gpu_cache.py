@@ -184,6 +184,22 @@ def test_lengths_far_below_their_bound(batch, q_len):
             Step((4, 2, 64), lengths, q_len, seed=31, max_len=max_len, slack=0).run_and_check()
 
 
+@pytest.mark.parametrize("batch", [1, 64, 200, 257])
+@pytest.mark.parametrize("q_len", [1, 9])
+def test_every_weight_repeats(batch, q_len):
+    """Slots that are not written keep what they held (-5), so that whole tables can be compared; caches in several ranges."""
+    lengths = [int(x) for x in np.exp(np.random.default_rng(batch).uniform(0, 6, batch))]
+    lengths[0], lengths[batch // 2] = 2100, 1303
+    s = Step((4, 2, 64), lengths, q_len, seed=31, max_len=2500)
+    s.run_and_check()
+    o, weight = s.o.clone(), s.weight_out.clone()
+    for _ in range(3):
+        s.weight_out.fill_(-5.0)
+        s.ws.fill_(255)
+        s.run()
+        assert torch.equal(s.o, o) and torch.equal(s.weight_out, weight)
+
+
 @pytest.mark.parametrize("heads,batch,q_len,prefix", [((32, 8, 128), 33, 4, 5000), ((32, 8, 128), 70, 9, 1000), ((8, 2, 64), 300, 1, 17000)])
 def test_long_caches_behind_a_prefix_of_much_work(heads, batch, q_len, prefix):
     """The prefix by shared tiles and the caches in several ranges, by the lengths and, above 256 requests, by their bound."""
