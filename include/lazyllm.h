@@ -557,6 +557,9 @@ typedef struct lazyllm_kv_cache {
  *   weight,   fp32 [batch, capacity], both or neither: weight_out[b][s] = weight[b][s] + sum over the new tokens of
  *   weight_out  the mean over all heads of their attention probability at slot s (Eq. 1), for a new token's own
  *             slot without the first term.  Slots beyond the new length are not written.  May be the same table.
+ *             What the new tokens add is one sum: where some of them (drafted ones) may be rejected, leave the
+ *             weights out of the call that verifies them, and add those of the accepted ones by one that has only
+ *             them, with q_len their number, for the requests that accepted as many (the lengths of the others negative).
  *   pos_new,  both or neither: pos_new int32 [batch] is the original position of a request's first new token; the
  *   pos       new tokens' positions are written into pos int32 [batch, capacity].
  *   prefix_*  lazyllm_op_prefix_attention only: K and V rows of prefix_len (up to 2^30) tokens that every request has

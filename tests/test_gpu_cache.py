@@ -472,6 +472,46 @@ def test_same_bits_every_time_and_on_another_stream():
             assert torch.equal(a.o, b.o) and torch.equal(a.weight_out, b.weight_out)
 
 
+@pytest.mark.parametrize("prefix", [0, 300])
+def test_weights_of_the_accepted_among_drafted_tokens(prefix):
+    """As the header says: verified without weights, then those of the accepted tokens alone, for the requests that accepted as
+    many together.  The tables are those of a step that had the accepted tokens only."""
+    lengths, accepted = [100, 0, 257, -1, 33, 700, 8], [5, 2, 0, 0, 2, 1, 5]
+    s = Step((4, 2, 64), lengths, 5, prefix=prefix, seed=27)
+    k, v, weight = s.k.clone(), s.v.clone(), s.weight.clone()
+    s.weights = False
+    s.run_and_check()                                           # verifies, in the same workspace
+    verified = s.o.clone()
+    s.k.copy_(k), s.v.copy_(v)                                  # (what the expectation of fewer tokens starts from)
+    for count in sorted(set(accepted) - {0}):
+        t = Step((4, 2, 64), [n if a == count else -1 for n, a in zip(lengths, accepted)], count, prefix=prefix, seed=27, max_len=700)
+        for x in ("q", "k_new", "v_new"):
+            getattr(t, x).copy_(getattr(s, x)[:, :count])
+        t.k[:, :700], t.v[:, :700], t.weight[:, :700], t.pk, t.pv = k[:, :700], v[:, :700], weight[:, :700], s.pk, s.pv
+        *_, add, reach = t.expected()
+        # the call itself: the caches and tables of the verification, a scratch o
+        o = torch.empty_like(t.q)
+        more = dict(weight=s.weight, weight_out=s.weight)
+        args = (t.q, t.k_new, t.v_new, t.len_dev, 4, count, s.max_len, o, s.ws)
+        if prefix:
+            B.lazyllm_op_prefix_attention(s.cache, s.pk, s.pv, *args, **more)
+        else:
+            B.lazyllm_op_cache_attention(s.cache, *args, **more)
+        torch.cuda.synchronize()
+        rel = 2 * 68 * 2.0 ** -24 * max(reach, 1.0) + 2.0 ** -16 + 1100 * 2.0 ** -24
+        for b, (n, a) in enumerate(zip(lengths, accepted)):
+            if a != count:
+                continue
+            want = torch.cat([weight[b, :n], torch.zeros(a, device=DEV)]).double() + add[b, :n + a]
+            assert bool(((s.weight[b, :n + a].double() - want).abs() <= add[b, :n + a] * rel + want * 2.0 ** -23 + 1e-30).all())
+            # the same rows as the verification's, up to the order of their sums and two roundings
+            assert torch.allclose(o[b].float(), verified[b, :a].float(), rtol=2.0 ** -7, atol=1e-3)
+    for b, (n, a) in enumerate(zip(lengths, accepted)):
+        assert torch.equal(s.weight[b, n + a:].isnan(), weight[b, n + a:].isnan())
+        if a == 0 and n >= 0:
+            assert torch.equal(s.weight[b, :n], weight[b, :n])
+
+
 @pytest.mark.parametrize("heads,lengths,prefix", [((4, 2, 64), [100, 0, 257, -1], 0), ((4, 2, 64), [100, 0, 257, -1], 300), ((8, 1, 128), [20, 5, 33, -1], 400),
                                                   ((32, 1, 128), [3] * 140, 5000)])
 def test_captured_step_replays_as_the_lengths_grow(heads, lengths, prefix):
