@@ -67,7 +67,9 @@ __device__ __forceinline__ uint32_t pack_halves(uint32_t hi, uint32_t lo, bool u
 // A wave takes 32 keys at a time, the four waves of a workgroup in turn over the range; both products run on 16x16x32 MFMAs,
 // transposed so that a lane owns a query column: S^T = K Q^T, O^T = V^T P^T.
 //   K: row by row into 32 rows of LDS that are the wave's own (no barrier: the copies of the next step start when this
-//      step's operands have been read), read as operands: lane (c = lane % 16, g = lane / 16) takes dimensions
+//      step's operands have been read, and have this step's first product and softmax to land in: they stand under a
+//      condition, so the compiler, which cannot count them, waits for all that is under way, logit stores too, in front
+//      of the second product), read as operands: lane (c = lane % 16, g = lane / 16) takes dimensions
 //      32 s + 8 g .. + 7 of key c.  Straight into operand registers, 64 bytes of 16 rows a load, was level without and 10 %
 //      slower with non-temporal loads (113.7 against 101 us below).
 //   V: straight into registers.  Lane (c, g) holds dimensions HD/16 c .. of the eight keys that its S^T accumulators belong
@@ -148,7 +150,7 @@ __global__ void __launch_bounds__(256, 2) cache_attention_kernel(CacheAttentionA
   it.tok0 = b * a.q_len;
   it.n_rows = (it.own ? 1 : a.batch) * a.q_len * a.group;
 
-  // (on its way while the length is)
+  // (on its way while the length is, where the request was not found from the lengths above)
   bf16x8_t qf[T][KS];
   int tok[T];
   size_t out_row[T];

@@ -6,9 +6,10 @@
 // the rows that have to move move (one per step in a cache that is full), no source is another row's destination, and
 // attention does not depend on the order of the slots (positions move along).
 //
-// One workgroup per request selects (latency bound: a few KB of tables, some ten barriers), a second launch moves the
-// rows of K and V at the rate of a copy; where the caches have room for a few evictions only, the selecting workgroup
-// moves them itself.  Where only a few tokens leave, as in a cache that is full, they are found directly.
+// Up to 16384 slots one workgroup per request selects (latency bound: a few KB of tables, some ten barriers), and a second
+// launch moves the rows of K and V at the rate of a copy; where the caches have room for a few evictions only, the
+// selecting workgroup moves them itself.  Where only a few tokens leave, as in a cache that is full, it finds them
+// directly.  From more slots many workgroups select, six launches for any number of tokens that leave.
 #include "common.h"
 
 namespace lz {
@@ -599,7 +600,9 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
 }
 
 // The largest capacity that one workgroup selects from (its registers end here): so far its launch is the quicker form, or as
-// quick (one request of 16000 27.9 us, the launches of the long form 28.3; of 9000 21.6 / 26.5; eight of 16000 47.4 / 49.3).
+// quick.  One workgroup / many, in us, a quarter of the slots kept: one request of 4096 16.5 / 25.2, 8192 21.0 / 26.4, 16384 31.3 /
+// 30.1; eight 25.0 / 35.3, 37.0 / 43.2, 63.0 / 63.2; 32 54 / 65, 104 / 113, 193 / 195; 16100 of 16384 kept 28.7 / 26.3, 31.1 / 30.8,
+// 42.0 / 46.8.  Where one token leaves the limit costs most: one request of 16384 10.4, of 16400 25.8; 32 requests 11.2, 35.2.
 constexpr int SELECT_CAPACITY = 16384;
 
 static size_t move_bytes(int batch, int capacity, int budget) {
