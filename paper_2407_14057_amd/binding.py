@@ -497,7 +497,7 @@ def _operand(t, here: int, dtype: torch.dtype, count: int) -> int:
 
 
 def _status(t, here: int) -> Optional[int]:
-    return None if t is None else _operand(t, here, torch.int32, 1 if type(t) is int else max(1, t.numel()))
+    return None if t is None else _operand(t, here, torch.int32, max(1, t.numel()) if isinstance(t, torch.Tensor) else 1)
 
 
 def _room(workspace: torch.Tensor) -> Tuple[int, int]:
@@ -512,13 +512,16 @@ def _step(cache, q, k_new, v_new, lengths, n_heads, q_len, max_len, o, here, pre
     rows, new, bf16, i32, f32 = (batch * q_len * n_heads * cache.head_dim, batch * q_len * cache.n_kv_heads * cache.head_dim, torch.bfloat16,
                                  torch.int32, torch.float32)
     # (packed at once: the constructor takes twice as long for its 17 members; 0 is NULL)
-    return lazyllm_step_attention.from_buffer_copy(_STEP_LAYOUT.pack(
-        _operand(q, here, bf16, rows), _operand(k_new, here, bf16, new), _operand(v_new, here, bf16, new), _operand(o, here, bf16, rows),
-        _operand(lengths, here, i32, batch), n_heads, q_len, max_len, prefix_len, prefix_k, prefix_v, prefix_stride,
-        0 if weight is None else _operand(weight, here, f32, slots),
-        0 if weight_out is None else _operand(weight_out, here, f32, slots),
-        0 if pos_new is None else _operand(pos_new, here, i32, batch),
-        0 if pos is None else _operand(pos, here, i32, slots), _status(status, here) or 0))
+    try:
+        return lazyllm_step_attention.from_buffer_copy(_STEP_LAYOUT.pack(
+            _operand(q, here, bf16, rows), _operand(k_new, here, bf16, new), _operand(v_new, here, bf16, new), _operand(o, here, bf16, rows),
+            _operand(lengths, here, i32, batch), n_heads, q_len, max_len, prefix_len, prefix_k, prefix_v, prefix_stride,
+            0 if weight is None else _operand(weight, here, f32, slots),
+            0 if weight_out is None else _operand(weight_out, here, f32, slots),
+            0 if pos_new is None else _operand(pos_new, here, i32, batch),
+            0 if pos is None else _operand(pos, here, i32, slots), _status(status, here) or 0))
+    except struct.error:                      # (a number that its member does not hold)
+        raise LazyLLMError(LAZYLLM_EINVAL) from None
 
 
 def lazyllm_op_cache_attention_workspace_bytes(cache: lazyllm_kv_cache, n_heads: int, q_len: int, max_len: int,
@@ -563,6 +566,8 @@ def lazyllm_op_cache_evict(cache, weight, pos, lengths, budget, sinks, recent, w
     """Tensors as the header documents them: contiguous, of those types and sizes, on the current device."""
     on = _cache_stream(cache, workspace, stream)
     here, batch, slots, i32, f32 = workspace.get_device(), cache.batch, cache.batch * cache.capacity, torch.int32, torch.float32
+    if sinks < 0 or recent < 0 or not sinks + recent <= budget < 1 << 31:          # (beyond that they would be cut to 32 bits)
+        raise LazyLLMError(LAZYLLM_EINVAL)
     _check(lib().lazyllm_op_cache_evict(
         C.byref(cache), _operand(weight, here, f32, slots), _operand(pos, here, i32, slots), _operand(lengths, here, i32, batch), budget, sinks,
         recent, _operand(weight_out, here, f32, slots), _operand(pos_out, here, i32, slots), _operand(lengths_out, here, i32, batch),

@@ -320,3 +320,29 @@ def test_blocks_of_query_rows_behind_a_prefix():
         assert ask(C.byref(_cache()), n_heads, q_len, prefix) == B.LAZYLLM_EINVAL
     assert ask(None, 4, 2, 100) == B.LAZYLLM_EINVAL
     assert ask(C.byref(_cache()), 4, 2, 1 << 30) == 16                 # (12 rows; a block of 256 would be nearly empty)
+
+
+def test_numbers_beyond_32_bits_are_refused(monkeypatch):
+    """Cut to 32 bits, a bound or budget of 2^32 + 5 would be 5."""
+    library = _Library(B.lib())
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    monkeypatch.setattr(B, "_lib_handle", library)
+
+    class Stream:
+        device_index, cuda_stream = -1, 77
+
+    ws = torch.zeros(4096, dtype=torch.uint8)
+    cache, t = _operands()
+    far = (1 << 32) + 5
+    tables = (t["weight"], t["pos"], t["lengths"])
+    outs = (t["weight_out"], t["pos_out"], t["lengths_out"], ws)
+    for call in (lambda: B.lazyllm_op_cache_attention(cache, t["q"], t["k_new"], t["v_new"], t["lengths"], 4, 2, far, t["o"], ws, stream=Stream),
+                 lambda: B.lazyllm_op_cache_attention(cache, t["q"], t["k_new"], t["v_new"], t["lengths"], 4, 2, -far, t["o"], ws, stream=Stream),
+                 lambda: B.lazyllm_op_cache_evict(cache, *tables, far, 1, 1, *outs, stream=Stream),
+                 lambda: B.lazyllm_op_cache_evict(cache, *tables, 5, far, 1 - far, *outs, stream=Stream),
+                 lambda: B.lazyllm_op_cache_evict(cache, *tables, 5, 1, far, *outs, stream=Stream),
+                 lambda: B.lazyllm_op_cache_evict(cache, *tables, 5, 1, 1, *outs, status="text", stream=Stream)):
+        with pytest.raises(B.LazyLLMError) as e:
+            call()
+        assert e.value.status == B.LAZYLLM_EINVAL
+    assert library.reached == 0
